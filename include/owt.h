@@ -263,6 +263,62 @@ owt_status owt_scale_hyperparameters(double k, double eps, double omega, double 
 owt_status owt_logistic_xent(int N, int O_local, int col_offset, owt_dtype dtype, const void *z, const int *labels,
                              float scale, float *loss, void *dz, void *hip_stream);
 
+/* ---- Rows of 8-bit values, and the dense shard on them ----
+ *
+ * q[r][c] * scale[r] stands for the real x[r][c]: whole numbers of -127 .. 127 with one fp32 scale a row.  A row of `cols` values takes
+ * owt_q8_pitch(cols) bytes, the next multiple of 128, with zeros behind its values (every call that writes rows writes them; a caller that
+ * brings rows of its own has to).  Rows serve as operands of the dense shard (activations, one scale a token; weights, one a channel),
+ * and as a checkpoint of what its backward pass reads: a byte a value instead of two or four.
+ * In these calls rows == 0 (or N == 0 in a descriptor) is an empty batch: nothing is written but what a sum over no rows gives. */
+size_t owt_q8_pitch(int cols);          /* 0 for cols <= 0 */
+
+/* Rows of x [rows][cols] in `dtype` to 8 bits: scale = max|x| / 127, q = x * 127 / max|x| to the nearest whole number, ties to even.  A row
+ * of zeros has scale 0.  A row that holds an infinity or a NaN has q = 0 and a scale that is not finite, so that it reads back as NaN.
+ * Errors: rows < 0, cols <= 0, unknown dtype, NULL or misaligned pointers -> OWT_EINVAL. */
+owt_status owt_q8_pack(int rows, int cols, owt_dtype dtype, const void *x, signed char *q, float *scale, void *hip_stream);
+
+/* Reads rows back: x[r][c] = q[r][c] * scale[r], stored in `dtype`. */
+owt_status owt_q8_unpack(int rows, int cols, owt_dtype dtype, const signed char *q, const float *scale, void *x, void *hip_stream);
+
+/* RMS norm of the residual stream, in 8 bits:
+ *     h = x + res,   rstd[r] = 1 / sqrt(mean_c h^2 + eps),   row r of (q, scale) = 8-bit row of h * gain * rstd
+ * x, res, h [rows][cols] in `dtype`; gain [cols], rstd [rows], scale [rows] fp32.  res may be NULL (h = x; h_or_null has to be NULL then),
+ * gain too (all ones), h too (the sum is not wanted), rstd too (no backward pass follows).  h may be x or res.  The norm is of the
+ * sum in fp32, h is the sum rounded to `dtype`.  cols <= 32768 (OWT_EUNSUPPORTED); the squares' sum has to fit fp32. */
+owt_status owt_rmsnorm_q8_fwd(int rows, int cols, owt_dtype dtype, const void *x, const void *res_or_null, const float *gain_or_null, float eps,
+                              void *h_or_null, signed char *q, float *scale, float *rstd_or_null, void *hip_stream);
+
+/* Its backward pass, the rounding to 8 bits taken as the identity.  With xn = h * rstd:
+ *     dh = rstd * (gain * dy - xn * mean_c(gain * dy * xn)) + dres,    dgain[c] = alpha * sum_r dy * xn + beta * dgain[c]
+ * dy is the gradient of the normed rows, dres that which arrives along the residual path (may be NULL); dh is the gradient of h, hence of
+ * x and of res alike, and may be dy or dres.  dy, h, dres, dh in `dtype`.  dgain_or_null NULL skips it (ws is not used then); beta == 0
+ * overwrites without reading.  ws: owt_rmsnorm_q8_workspace_bytes. */
+owt_status owt_rmsnorm_q8_bwd(int rows, int cols, owt_dtype dtype, const void *dy, const void *h, const float *gain_or_null, const float *rstd,
+                              const void *dres_or_null, float alpha, float beta, void *dh, float *dgain_or_null, void *ws, size_t ws_bytes,
+                              void *hip_stream);
+size_t owt_rmsnorm_q8_workspace_bytes(int rows, int cols);      /* (size_t)-1 on bad sizes */
+
+/* The dense shard of owt_fc_shard_fwd on 8-bit rows (O_local = O_total / workers):
+ *     y[n][o] = act(xscale[n] * wscale[o] * sum_i xq[n][i] * wq[o][i] + bias[o])
+ * xq [N] rows and wq [O_local] rows of I values at owt_q8_pitch(I) bytes; y [N][O_local] in the descriptor's dtype; bias fp32, read only
+ * with OWT_BIAS.  The sum is exact.  I <= 131071, N and O_local <= 2^22 (OWT_EUNSUPPORTED). */
+owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
+                               const float *bias, void *y, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* Backward pass of the shard from its 8-bit checkpoint, as owt_fc_shard_bwd with x and w read as the values their rows stand for:
+ *     dz = dy * [y > 0] with OWT_RELU (y required), else dy
+ *     dx_partial[n][i] = sum_o dz[n][o] * wscale[o] * wq[o][i]                     (NULL to skip)
+ *     dw[o][i] = alpha * sum_n dz[n][o] * xscale[n] * xq[n][i] + beta * dw;   dbias[o] = alpha * sum_n dz[n][o] + beta * dbias   (NULL to skip)
+ * dy, y [N][O_local], dx_partial [N][I] in the descriptor's dtype; dw [O_local][I] (dense, no pitch) and dbias fp32.
+ * dz times its scale is multiplied as the sum of two f16 values under a power of two for each row of a result, which hold 22 bits of all
+ * that is within 2^-16 of the row's largest such value, and 2^-39 of the largest below that; one f16 value (11 bits) for dx in bf16.
+ * ws: owt_fc_shard_q8_workspace_bytes of OWT_PASS_BWD_DATA (one figure for the whole pass), about 2 to 4 bytes for every value of xq and
+ * wq and 2 to 8 for every value of dz. */
+owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
+                               const void *y_or_null, const void *dy, float alpha, float beta, void *dx_partial_or_null, float *dw,
+                               float *dbias_or_null, void *ws, size_t ws_bytes, void *hip_stream);
+size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass);     /* (size_t)-1 on a bad descriptor */
+
 /* Message for the calling thread's most recent non-OK return ("" if none).
  * Points at thread-local static storage; valid until the thread's next call. */
 const char *owt_last_error(void);
@@ -281,7 +337,7 @@ const char *owt_last_error(void);
  * 71 its forward pass in one launch; bf16 of any channel counts:
  * 80..86 stride-1 filter gradient, 87..89 filter gradient of any geometry, 90 forward / backward-data and strided
  * forward, 92..94 forward / backward-data of layers of few tiles; 100..106 the bf16 filter gradient over images
- * that streams its operands into LDS), `splitk` > 0 forces the
+ * that streams its operands into LDS; 110..112 the products of the dense shard in 8 bits), `splitk` > 0 forces the
  * split count of the reduction (clamped to the number of reduction steps), `flags` is a set of
  * OWT_FORCE_* bits.  While an override is active, tuned and cached plans are ignored.  The three
  * values are stored atomically, but a launch that runs concurrently with this call may see the old

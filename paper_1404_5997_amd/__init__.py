@@ -28,6 +28,8 @@ EXPORTS = (
     "owt_conv_bwd_data_relu_in", "owt_maxpool_bwd_relu", "owt_sgd_momentum_update", "owt_scale_hyperparameters",
     "owt_logistic_xent", "owt_fc_autotune", "owt_test_force_variant",
     "owt_conv_bwd_filter_static", "owt_static_scratch_bytes",
+    "owt_q8_pitch", "owt_q8_pack", "owt_q8_unpack", "owt_rmsnorm_q8_fwd", "owt_rmsnorm_q8_bwd", "owt_rmsnorm_q8_workspace_bytes",
+    "owt_fc_shard_q8_fwd", "owt_fc_shard_q8_bwd", "owt_fc_shard_q8_workspace_bytes",
 )
 
 
@@ -76,6 +78,18 @@ _d = ctypes.c_double
 _lib.owt_sgd_momentum_update.argtypes = [_sz, _vp, _vp, _vp, _f, _f, _f, _f, _vp, _vp]
 _lib.owt_scale_hyperparameters.argtypes = [_d, _d, _d, ctypes.POINTER(_d), ctypes.POINTER(_d)]
 _lib.owt_logistic_xent.argtypes = [_i, _i, _i, _i, _vp, _vp, _f, _vp, _vp, _vp]
+_lib.owt_q8_pitch.restype = _sz
+_lib.owt_q8_pitch.argtypes = [_i]
+_lib.owt_q8_pack.argtypes = [_i, _i, _i, _vp, _vp, _vp, _vp]
+_lib.owt_q8_unpack.argtypes = [_i, _i, _i, _vp, _vp, _vp, _vp]
+_lib.owt_rmsnorm_q8_fwd.argtypes = [_i, _i, _i, _vp, _vp, _vp, _f, _vp, _vp, _vp, _vp, _vp]
+_lib.owt_rmsnorm_q8_bwd.argtypes = [_i, _i, _i, _vp, _vp, _vp, _vp, _vp, _f, _f, _vp, _vp, _vp, _sz, _vp]
+_lib.owt_rmsnorm_q8_workspace_bytes.restype = _sz
+_lib.owt_rmsnorm_q8_workspace_bytes.argtypes = [_i, _i]
+_lib.owt_fc_shard_q8_fwd.argtypes = [_fd, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.owt_fc_shard_q8_bwd.argtypes = [_fd, _vp, _vp, _vp, _vp, _vp, _vp, _f, _f, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.owt_fc_shard_q8_workspace_bytes.restype = _sz
+_lib.owt_fc_shard_q8_workspace_bytes.argtypes = [_fd, _i]
 _lib.owt_last_error.restype = ctypes.c_char_p
 _lib.owt_abi_version.restype = _i
 _lib.owt_conv_plan_describe.argtypes = [_cd, _i, ctypes.c_char_p, _sz]
@@ -257,3 +271,53 @@ def owt_logistic_xent(N, O_local, col_offset, dtype, z, labels, scale, loss, dz,
 def owt_maxpool_bwd_relu(N, H, W, C, win, stride, dtype, dy, argmax, y_pooled, dx, stream=None):
     _check(_lib.owt_maxpool_bwd_relu(N, H, W, C, win, stride, dtype, _ptr(dy), _ptr(argmax), _ptr(y_pooled), _ptr(dx),
                                      _stream(stream)))
+
+
+def owt_q8_pitch(cols):
+    return _lib.owt_q8_pitch(cols)
+
+
+def owt_q8_pack(rows, cols, dtype, x, q, scale, stream=None):
+    _check(_lib.owt_q8_pack(rows, cols, dtype, _ptr(x), _ptr(q), _ptr(scale), _stream(stream)))
+
+
+def owt_q8_unpack(rows, cols, dtype, q, scale, x, stream=None):
+    _check(_lib.owt_q8_unpack(rows, cols, dtype, _ptr(q), _ptr(scale), _ptr(x), _stream(stream)))
+
+
+def owt_rmsnorm_q8_fwd(rows, cols, dtype, x, res_or_null, gain_or_null, eps, h_or_null, q, scale, rstd_or_null=None, stream=None):
+    _check(_lib.owt_rmsnorm_q8_fwd(rows, cols, dtype, _ptr(x), _ptr(res_or_null), _ptr(gain_or_null), eps, _ptr(h_or_null), _ptr(q),
+                                   _ptr(scale), _ptr(rstd_or_null), _stream(stream)))
+
+
+def owt_rmsnorm_q8_workspace_bytes(rows, cols):
+    n = _lib.owt_rmsnorm_q8_workspace_bytes(rows, cols)
+    if n == ctypes.c_size_t(-1).value:
+        raise OwtError(OWT_EINVAL, owt_last_error())
+    return n
+
+
+def owt_rmsnorm_q8_bwd(rows, cols, dtype, dy, h, gain_or_null, rstd, dres_or_null, alpha, beta, dh, dgain_or_null, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_lib.owt_rmsnorm_q8_bwd(rows, cols, dtype, _ptr(dy), _ptr(h), _ptr(gain_or_null), _ptr(rstd), _ptr(dres_or_null), alpha, beta,
+                                   _ptr(dh), _ptr(dgain_or_null), p, n, _stream(stream)))
+
+
+def owt_fc_shard_q8_workspace_bytes(desc, pass_):
+    n = _lib.owt_fc_shard_q8_workspace_bytes(ctypes.byref(desc), pass_)
+    if n == ctypes.c_size_t(-1).value:
+        raise OwtError(OWT_EINVAL, owt_last_error())
+    return n
+
+
+def owt_fc_shard_q8_fwd(desc, xq, xscale, wq, wscale, bias, y, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_lib.owt_fc_shard_q8_fwd(ctypes.byref(desc), _ptr(xq), _ptr(xscale), _ptr(wq), _ptr(wscale), _ptr(bias), _ptr(y), p, n,
+                                    _stream(stream)))
+
+
+def owt_fc_shard_q8_bwd(desc, xq, xscale, wq, wscale, y_or_null, dy, alpha, beta, dx_partial_or_null, dw, dbias_or_null, ws=None,
+                        stream=None):
+    p, n = _ws(ws)
+    _check(_lib.owt_fc_shard_q8_bwd(ctypes.byref(desc), _ptr(xq), _ptr(xscale), _ptr(wq), _ptr(wscale), _ptr(y_or_null), _ptr(dy), alpha,
+                                    beta, _ptr(dx_partial_or_null), _ptr(dw), _ptr(dbias_or_null), p, n, _stream(stream)))

@@ -532,6 +532,8 @@ static bool image_groups_fit(const Geom &g, bool xgather)
 // What owt_test_force_variant asked for (tests only; -1 / 0 = the planner decides).
 static std::atomic<int> g_force_tile{-1}, g_force_split{-1};
 static std::atomic<unsigned> g_force_flags{0};
+int forced_tile() { return g_force_tile.load(std::memory_order_relaxed); }
+int forced_split() { return g_force_split.load(std::memory_order_relaxed); }
 static inline bool forced(unsigned bit) { return (g_force_flags.load(std::memory_order_relaxed) & bit) != 0; }
 
 static void enumerate(const Geom &g, int pass, const PassDims &dm, bool want_db, std::vector<Launch> &out, std::vector<Demand> *demand = nullptr)

@@ -12,6 +12,8 @@ namespace owt {
 
 owt_status fail(owt_status st, const char *fmt, ...);
 void clear_error();
+int forced_tile();          // what owt_test_force_variant set, or -1
+int forced_split();
 
 inline bool aligned16(const void *p) { return (((uintptr_t)p) & 15u) == 0; }
 

@@ -1,0 +1,235 @@
+// The fully-connected column shard in 8 bits: entry points of q8gemm.hpp and q8prep.hpp.
+#include <cmath>
+#include <initializer_list>
+
+#include "owt_host.hpp"
+#include "q8.hpp"
+#include "q8gemm.hpp"
+#include "q8prep.hpp"
+
+namespace owt {
+
+struct Q8Tile { int bm, bn, occ; float step_us, start_us; };
+constexpr int kNumQ8Tiles = 3, kQ8FirstTile = 110;      // owt_test_force_variant: tile numbers 110.. name these
+// microseconds of a step of a work-group on a full chip, and of its start and end
+static const Q8Tile kQ8Tiles[kNumQ8Tiles] = {{256, 256, 1, 1.6f, 4.f}, {128, 128, 1, 0.6f, 2.5f}, {64, 64, 2, 0.5f, 2.f}};
+
+template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, hipStream_t s)
+{
+    const dim3 grid((unsigned)owt_split_major_grid(p.tiles, p.splits));
+    if (t == 0) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 4, 4, 2, 2, 1>), grid, dim3(512), 0, s, p);
+    else if (t == 1) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 2, 2, 3, 1>), grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 1, 1, 4, 2>), grid, dim3(256), 0, s, p);
+    return hipGetLastError();
+}
+
+struct Q8Plan { int tile, splits; };
+static Q8Plan q8_plan(long M, long N, int ksteps)
+{
+    Q8Plan best{0, 1};
+    float least = 1e30f;
+    const int want = forced_tile() - kQ8FirstTile, want_split = forced_split();
+    for (int t = 0; t < kNumQ8Tiles; t++) {
+        if (want >= 0 && want < kNumQ8Tiles && t != want) continue;
+        const Q8Tile &q = kQ8Tiles[t];
+        const long tiles = ((M + q.bm - 1) / q.bm) * ((N + q.bn - 1) / q.bn);
+        for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= ksteps && tiles * sp <= 1024)); sp *= 2) {
+            const long rounds = (tiles * sp + 256 * q.occ - 1) / (256 * q.occ);
+            float us = (float)rounds * ((float)((ksteps + sp - 1) / sp) * q.step_us + q.start_us);
+            if (sp > 1) us += 4.f + (float)(sp + 1) * (float)M * (float)N * 4e-6f / 4.f;
+            if (us < least) { least = us; best = {t, sp}; }
+        }
+    }
+    if (want_split > 0) best.splits = want_split < ksteps ? want_split : ksteps;
+    return best;
+}
+
+static size_t partial_bytes(const Q8Plan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
+
+template <class Op> static owt_status run_product(Q8GemmParams p, const Q8Plan &pl, void *partial, hipStream_t s)
+{
+    const Q8Tile &q = kQ8Tiles[pl.tile];
+    p.tiles_n = (p.N + q.bn - 1) / q.bn;
+    const long tiles = (long)p.tiles_n * ((p.M + q.bm - 1) / q.bm);
+    if (tiles * pl.splits > 0x3fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+    p.tiles = (int)tiles;
+    p.splits = pl.splits;
+    p.ksteps_per_split = ((p.ksteps / p.planes + pl.splits - 1) / pl.splits) * p.planes;
+    p.partial = partial;
+    hipError_t e = launch_tile<Op>(pl.tile, p, s);
+    if (e == hipSuccess && pl.splits > 1) {
+        const size_t n = (size_t)p.M * p.N, want = (n + 255) / 256;
+        hipLaunchKernelGGL(q8_join_kernel<decltype(typename Op::Acc()[0] + 0)>, dim3((unsigned)(want < 8192 ? want : 8192)), dim3(256), 0, s, p);
+        e = hipGetLastError();
+    }
+    return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+}
+
+constexpr int kQ8MaxI = 131071;         // 128 * 128 * 131071 < 2^31: no sum of products leaves 32 bits
+
+static owt_status check_q8_fc(const owt_fc_desc *d, int &o_local)
+{
+    if (!d) return fail(OWT_EINVAL, "descriptor is NULL");
+    if (d->N < 0 || d->I <= 0 || d->O_total <= 0 || d->workers <= 0)
+        return fail(OWT_EINVAL, "N must not be negative; I, O_total and workers must be positive");
+    if (d->rank < 0 || d->rank >= d->workers) return fail(OWT_EINVAL, "need 0 <= rank < workers");
+    if (d->O_total % d->workers) return fail(OWT_EINVAL, "O_total must be divisible by workers");
+    if (d->dtype != OWT_F32 && d->dtype != OWT_BF16) return fail(OWT_EINVAL, "unknown dtype %d", (int)d->dtype);
+    if (d->flags & ~(unsigned)(OWT_BIAS | OWT_RELU)) return fail(OWT_EINVAL, "unknown flag bits 0x%x", d->flags);
+    o_local = d->O_total / d->workers;
+    if (d->I > kQ8MaxI) return fail(OWT_EUNSUPPORTED, "more than %d inputs", kQ8MaxI);
+    if (d->N > (1 << 22) || o_local > (1 << 22)) return fail(OWT_EUNSUPPORTED, "more than 2^22 rows or columns");
+    return OWT_OK;
+}
+static owt_status need_ptr(const void *p, const char *what)
+{
+    if (!p) return fail(OWT_EINVAL, "%s is NULL", what);
+    return aligned16(p) ? OWT_OK : fail(OWT_EINVAL, "%s is not 16-byte aligned", what);
+}
+static owt_status may_ptr(const void *p, const char *what) { return aligned16(p) ? OWT_OK : fail(OWT_EINVAL, "%s is not 16-byte aligned", what); }
+static owt_status need_ws(const void *ws, size_t have, size_t need)
+{
+    if (have < need) return fail(OWT_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, have);
+    if (need && (!ws || !aligned16(ws))) return fail(OWT_EINVAL, "ws is NULL or misaligned");
+    return OWT_OK;
+}
+
+// The backward pass's scratch, laid out in order; `take` returns the offset of each part.
+struct Q8BwdLayout {
+    int nk, ok, strips, strip_rows, planes;
+    Q8Plan dw, dx;
+    size_t colsum, colmax, rowmax, cexp, rexp, aw, ax, bw, bx, partial, total;
+    Q8BwdLayout(int N, int I, int O, bool bf16)
+    {
+        nk = N > 0 ? (N + 63) / 64 : 1;
+        ok = (O + 63) / 64;
+        planes = bf16 ? 1 : 2;
+        // strips: enough parts of 64 columns for the chip, no more than 64 to add up
+        long want = (2048 + ok - 1) / ok;
+        want = want > 64 ? 64 : want;
+        long rows = (N + want - 1) / want;
+        rows = rows < 16 ? 16 : (rows + 3) / 4 * 4;
+        strip_rows = (int)rows;
+        strips = (int)((N + rows - 1) / rows);
+        dw = q8_plan(O, I, 2 * nk);
+        dx = q8_plan(N, I, planes * ok);
+        size_t at = 0;
+        auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
+        colsum = take((size_t)strips * O * 4);
+        colmax = take((size_t)strips * O * 4);
+        rowmax = take((size_t)ok * N * 4);
+        cexp = take((size_t)O * 4);
+        rexp = take((size_t)N * 4);
+        aw = take((size_t)O * nk * 256);
+        ax = take((size_t)N * ok * 128 * planes);
+        bw = take((size_t)I * nk * 128);
+        bx = take((size_t)I * ok * 128);
+        const size_t a = partial_bytes(dw, O, I), b = partial_bytes(dx, N, I);
+        partial = take(a > b ? a : b);
+        total = at;
+    }
+};
+
+}  // namespace owt
+
+using namespace owt;
+#define OWT_TRY(e) do { const owt_status st_ = (e); if (st_ != OWT_OK) return st_; } while (0)
+
+extern "C" {
+
+size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass)
+{
+    int ol;
+    if (pass < 0 || pass > 2) { fail(OWT_EINVAL, "pass must be 0, 1 or 2"); return (size_t)-1; }
+    if (check_q8_fc(d, ol) != OWT_OK) return (size_t)-1;
+    if (pass == OWT_PASS_FWD) {
+        if (d->N == 0) return 0;
+        const int ks = (int)(q8_pitch(d->I) / 128);
+        return partial_bytes(q8_plan(d->N, ol, ks), d->N, ol);
+    }
+    return Q8BwdLayout(d->N, d->I, ol, d->dtype == OWT_BF16).total;
+}
+
+owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
+                               const float *bias, void *y, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int ol;
+    OWT_TRY(check_q8_fc(d, ol));
+    if (d->N == 0) return OWT_OK;
+    OWT_TRY(need_ptr(xq, "xq")); OWT_TRY(need_ptr(xscale, "xscale")); OWT_TRY(need_ptr(wq, "wq")); OWT_TRY(need_ptr(wscale, "wscale"));
+    OWT_TRY(need_ptr(y, "y"));
+    if (d->flags & OWT_BIAS) OWT_TRY(need_ptr(bias, "bias"));
+    const size_t pitch = q8_pitch(d->I);
+    const Q8Plan pl = q8_plan(d->N, ol, (int)(pitch / 128));
+    OWT_TRY(need_ws(ws, ws_bytes, partial_bytes(pl, d->N, ol)));
+    Q8GemmParams p;
+    memset(&p, 0, sizeof(p));
+    p.a = (const unsigned char *)xq; p.b = (const unsigned char *)wq;
+    p.lda = p.ldb = pitch;
+    p.M = d->N; p.N = ol; p.ksteps = (int)(pitch / 128); p.planes = 1;
+    p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, y, (d->flags & OWT_RELU) ? 1 : 0, d->dtype == OWT_BF16 ? 1 : 0};
+    return run_product<Q8Int>(p, pl, ws, (hipStream_t)hip_stream);
+}
+
+owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
+                               const void *y_or_null, const void *dy, float alpha, float beta, void *dx_partial_or_null, float *dw,
+                               float *dbias_or_null, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    int ol;
+    OWT_TRY(check_q8_fc(d, ol));
+    if (!std::isfinite(alpha) || !std::isfinite(beta)) return fail(OWT_EINVAL, "alpha and beta must be finite");
+    OWT_TRY(need_ptr(dw, "dw"));
+    OWT_TRY(need_ptr(wq, "wq")); OWT_TRY(need_ptr(wscale, "wscale"));
+    OWT_TRY(may_ptr(dx_partial_or_null, "dx_partial")); OWT_TRY(may_ptr(dbias_or_null, "dbias"));
+    if (d->N > 0) {
+        OWT_TRY(need_ptr(xq, "xq")); OWT_TRY(need_ptr(xscale, "xscale")); OWT_TRY(need_ptr(dy, "dy"));
+        if (d->flags & OWT_RELU) OWT_TRY(need_ptr(y_or_null, "y (needed for the ReLU mask)"));
+    }
+    const bool bf16 = d->dtype == OWT_BF16, want_dx = dx_partial_or_null && d->N > 0;
+    const Q8BwdLayout l(d->N, d->I, ol, bf16);
+    OWT_TRY(need_ws(ws, ws_bytes, l.total));
+    hipStream_t s = (hipStream_t)hip_stream;
+    char *at = (char *)ws;
+
+    Q8PrepParams q;
+    memset(&q, 0, sizeof(q));
+    q.dy = dy; q.y = (d->flags & OWT_RELU) ? y_or_null : nullptr;
+    q.xs = xscale; q.ws = wscale; q.xq = xq; q.wq = wq;
+    q.N = d->N; q.I = d->I; q.O = ol; q.bf16 = bf16; q.xpitch = q8_pitch(d->I);
+    q.want_dx = want_dx; q.dx_planes = l.planes;
+    q.alpha = alpha; q.beta = beta; q.db = dbias_or_null;
+    q.strips = l.strips; q.strip_rows = l.strip_rows;
+    q.colsum = (float *)(at + l.colsum); q.colmax = (float *)(at + l.colmax); q.rowmax = (float *)(at + l.rowmax);
+    q.col_exp = (int *)(at + l.cexp); q.row_exp = (int *)(at + l.rexp);
+    q.aw = (_Float16 *)(at + l.aw); q.ax = (_Float16 *)(at + l.ax); q.bw = (_Float16 *)(at + l.bw); q.bx = (_Float16 *)(at + l.bx);
+    q.nk = l.nk; q.ok = l.ok;
+    const long its = (d->I + 63) / 64, tz = (long)l.nk * l.ok, tx = its * l.nk, tw = want_dx ? its * l.ok : 0;
+    if (tz + tx + tw > 0x7fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 tiles of 64 x 64 values");
+    q.tiles_z = (int)tz; q.tiles_x = (int)tx;
+    if (l.strips > 0) {
+        const dim3 grid((unsigned)l.ok, (unsigned)l.strips);
+        if (bf16) hipLaunchKernelGGL(q8_stat_kernel<bf16_t>, grid, dim3(256), 0, s, q);
+        else hipLaunchKernelGGL(q8_stat_kernel<float>, grid, dim3(256), 0, s, q);
+    }
+    const dim3 grid((unsigned)(tz + tx + tw));
+    if (bf16) hipLaunchKernelGGL(q8_prep_kernel<bf16_t>, grid, dim3(256), 0, s, q);
+    else hipLaunchKernelGGL(q8_prep_kernel<float>, grid, dim3(256), 0, s, q);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+
+    Q8GemmParams p;
+    memset(&p, 0, sizeof(p));
+    p.a = (const unsigned char *)q.aw; p.b = (const unsigned char *)q.bw;
+    p.lda = (size_t)l.nk * 256; p.ldb = (size_t)l.nk * 128;
+    p.M = ol; p.N = d->I; p.ksteps = 2 * l.nk; p.planes = 2;
+    p.d = {q.col_exp, alpha, beta, dw, 0};
+    OWT_TRY(run_product<Q8Half>(p, l.dw, at + l.partial, s));
+    if (!want_dx) return OWT_OK;
+    p.a = (const unsigned char *)q.ax; p.b = (const unsigned char *)q.bx;
+    p.lda = (size_t)l.ok * 128 * l.planes; p.ldb = (size_t)l.ok * 128;
+    p.M = d->N; p.N = d->I; p.ksteps = l.planes * l.ok; p.planes = l.planes;
+    p.d = {q.row_exp, 1.f, 0.f, dx_partial_or_null, bf16 ? 1 : 0};
+    return run_product<Q8Half>(p, l.dx, at + l.partial, s);
+}
+
+}  // extern "C"
