@@ -17,7 +17,7 @@ static const Q8Tile kQ8Tiles[kNumQ8Tiles] = {{256, 256, 1, 1.6f, 4.f}, {128, 128
 template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, hipStream_t s)
 {
     const dim3 grid((unsigned)owt_split_major_grid(p.tiles, p.splits));
-    if (t == 0) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 4, 4, 2, 2, 1>), grid, dim3(512), 0, s, p);
+    if (t == 0) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 4, 4, 2, 1>), grid, dim3(256), 0, s, p);
     else if (t == 1) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 2, 2, 3, 1>), grid, dim3(256), 0, s, p);
     else hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 1, 1, 4, 2>), grid, dim3(256), 0, s, p);
     return hipGetLastError();
@@ -58,8 +58,8 @@ template <class Op> static owt_status run_product(Q8GemmParams p, const Q8Plan &
     p.partial = partial;
     hipError_t e = launch_tile<Op>(pl.tile, p, s);
     if (e == hipSuccess && pl.splits > 1) {
-        const size_t n = (size_t)p.M * p.N, want = (n + 255) / 256;
-        hipLaunchKernelGGL(q8_join_kernel<decltype(typename Op::Acc()[0] + 0)>, dim3((unsigned)(want < 8192 ? want : 8192)), dim3(256), 0, s, p);
+        const size_t n = (size_t)p.M * ((p.N + 3) / 4), want = (n + 255) / 256;
+        hipLaunchKernelGGL(q8_join_kernel<Op>, dim3((unsigned)(want < 8192 ? want : 8192)), dim3(256), 0, s, p);
         e = hipGetLastError();
     }
     return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
@@ -167,7 +167,8 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
     p.a = (const unsigned char *)xq; p.b = (const unsigned char *)wq;
     p.lda = p.ldb = pitch;
     p.M = d->N; p.N = ol; p.ksteps = (int)(pitch / 128); p.planes = 1;
-    p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, y, (d->flags & OWT_RELU) ? 1 : 0, d->dtype == OWT_BF16 ? 1 : 0};
+    p.out = y; p.bf16 = d->dtype == OWT_BF16;
+    p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, (d->flags & OWT_RELU) ? 1 : 0};
     return run_product<Q8Int>(p, pl, ws, (hipStream_t)hip_stream);
 }
 
@@ -222,13 +223,15 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     p.a = (const unsigned char *)q.aw; p.b = (const unsigned char *)q.bw;
     p.lda = (size_t)l.nk * 256; p.ldb = (size_t)l.nk * 128;
     p.M = ol; p.N = d->I; p.ksteps = 2 * l.nk; p.planes = 2;
-    p.d = {q.col_exp, alpha, beta, dw, 0};
+    p.out = dw; p.bf16 = 0;
+    p.d = {q.col_exp, alpha, beta};
     OWT_TRY(run_product<Q8Half>(p, l.dw, at + l.partial, s));
     if (!want_dx) return OWT_OK;
     p.a = (const unsigned char *)q.ax; p.b = (const unsigned char *)q.bx;
     p.lda = (size_t)l.ok * 128 * l.planes; p.ldb = (size_t)l.ok * 128;
     p.M = d->N; p.N = d->I; p.ksteps = l.planes * l.ok; p.planes = l.planes;
-    p.d = {q.row_exp, 1.f, 0.f, dx_partial_or_null, bf16 ? 1 : 0};
+    p.out = dx_partial_or_null; p.bf16 = bf16;
+    p.d = {q.row_exp, 1.f, 0.f};
     return run_product<Q8Half>(p, l.dx, at + l.partial, s);
 }
 

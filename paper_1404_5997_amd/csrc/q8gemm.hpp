@@ -13,6 +13,8 @@
 // 16-byte piece c of row r sits in slot c ^ ((r >> 1) & 7), which spreads a fragment's 32 rows over all banks.  Rows past the end of an
 // operand re-read its last one; their results are not stored.
 #pragma once
+#include <type_traits>
+
 #include "owt_common.hpp"
 
 namespace owt {
@@ -37,15 +39,12 @@ struct Q8Half {
 // Results of the forward pass: both scales, bias, ReLU, storage type
 struct Q8FwdOut {
     const float *xs, *ws, *bias;        // bias may be null
-    void *y;
-    int relu, bf16;
+    int relu;
 };
 // Results of a backward product: row m was scaled by 2^exps[m]
 struct Q8BwdOut {
     const int *exps;
-    float alpha, beta;
-    void *out;
-    int bf16;
+    float alpha, beta;                  // beta only where results are fp32
 };
 
 struct Q8GemmParams {
@@ -55,30 +54,92 @@ struct Q8GemmParams {
     int planes;                         // consecutive steps of A that meet the same step of B
     int tiles_n, splits, ksteps_per_split;
     int tiles;                          // tiles_m * tiles_n
+    void *out;                          // C
+    int bf16;                           // its type
     void *partial;                      // [splits][M][N], 32 bits each (splits > 1)
     Q8FwdOut f;
     Q8BwdOut d;
 };
 
-// The value of C[m][c] from its whole sum
-__device__ __forceinline__ void q8_finish(const Q8GemmParams &p, int m, int c, int sum)
+// Four results C[m][c .. c + 3] of a row of N.  VEC: N is a multiple of four (then c is, too, and rows are aligned to four values); without it
+// the last ones may be past the row.
+template <bool VEC, class T> __device__ __forceinline__ void q8_store4(T *row, int c, int N, const float (&v)[4])
 {
-    float v = (float)sum * (p.f.xs[m] * p.f.ws[c]);
-    if (p.f.bias) v += p.f.bias[c];
-    if (p.f.relu) v = fmaxf(v, 0.f);
-    const size_t o = (size_t)m * p.N + c;
-    if (p.f.bf16) store1((bf16_t *)p.f.y, o, v);
-    else store1((float *)p.f.y, o, v);
-}
-__device__ __forceinline__ void q8_finish(const Q8GemmParams &p, int m, int c, float sum)
-{
-    float v = ldexpf(sum, -p.d.exps[m]) * p.d.alpha;
-    const size_t o = (size_t)m * p.N + c;
-    if (p.d.bf16) store1((bf16_t *)p.d.out, o, v);
-    else {
-        if (p.d.beta != 0.f) v += p.d.beta * ((const float *)p.d.out)[o];
-        store1((float *)p.d.out, o, v);
+    if (VEC) {
+        if (c >= N) return;
+        if (sizeof(T) == 4) *(float4 *)((float *)row + c) = make_float4(v[0], v[1], v[2], v[3]);
+        else *(uint2 *)((uint16_t *)row + c) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; t++)
+            if (c + t < N) store1(row, (size_t)(c + t), v[t]);
     }
+}
+template <bool VEC> __device__ __forceinline__ void q8_load4(const float *row, int c, int N, float (&v)[4])
+{
+    if (VEC) {
+        const float4 u = c < N ? *(const float4 *)(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
+        v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; t++) v[t] = c + t < N ? row[c + t] : 0.f;
+    }
+}
+// What four columns have in common for all rows, and a row for all columns: its scale, or its exponent.
+struct Q8Cols { float ws[4], bias[4]; };
+__device__ __forceinline__ Q8Cols q8_cols(const Q8GemmParams &p, int c, q8_i32x16)
+{
+    Q8Cols k = {};
+    q8_load4<false>(p.f.ws, c, p.N, k.ws);
+    if (p.f.bias) q8_load4<false>(p.f.bias, c, p.N, k.bias);
+    return k;
+}
+__device__ __forceinline__ Q8Cols q8_cols(const Q8GemmParams &, int, q8_f32x16) { return {}; }
+__device__ __forceinline__ int q8_row(const Q8GemmParams &p, int m, q8_i32x16) { return m < p.M ? __float_as_int(p.f.xs[m]) : 0; }
+__device__ __forceinline__ int q8_row(const Q8GemmParams &p, int m, q8_f32x16) { return m < p.M ? p.d.exps[m] : 0; }
+
+// Results from whole sums
+__device__ __forceinline__ void q8_values(const Q8GemmParams &p, const Q8Cols &k, int row, const int (&sum)[4], float (&v)[4])
+{
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+        v[t] = (float)sum[t] * (__int_as_float(row) * k.ws[t]) + k.bias[t];
+        if (p.f.relu) v[t] = v[t] < 0.f ? 0.f : v[t];           // (NaN stays)
+    }
+}
+__device__ __forceinline__ void q8_values(const Q8GemmParams &p, const Q8Cols &, int row, const float (&sum)[4], float (&v)[4])
+{
+#pragma unroll
+    for (int t = 0; t < 4; t++) v[t] = ldexpf(sum[t], -row) * p.d.alpha;
+}
+// How results are written
+enum { Q8_PARTIAL, Q8_F32, Q8_F32_ADD, Q8_BF16 };
+template <int HOW, bool VEC> __device__ __forceinline__ void q8_put(const Q8GemmParams &p, int m, int c, float (&v)[4])
+{
+    if (HOW == Q8_BF16) q8_store4<VEC>((bf16_t *)p.out + (size_t)m * p.N, c, p.N, v);
+    else {
+        float *row = (float *)p.out + (size_t)m * p.N;
+        if (HOW == Q8_F32_ADD) {
+            float old[4];
+            q8_load4<VEC>(row, c, p.N, old);
+#pragma unroll
+            for (int t = 0; t < 4; t++) v[t] += p.d.beta * old[t];
+        }
+        q8_store4<VEC>(row, c, p.N, v);
+    }
+}
+// calls f(how, vec) with the constants of this product
+template <class F> __device__ __forceinline__ void q8_how(const Q8GemmParams &p, bool partial, F f)
+{
+    using std::integral_constant;
+    auto with = [&](auto vec) __attribute__((always_inline)) {
+        if (partial) f(integral_constant<int, Q8_PARTIAL>{}, vec);
+        else if (p.bf16) f(integral_constant<int, Q8_BF16>{}, vec);
+        else if (p.d.beta != 0.f) f(integral_constant<int, Q8_F32_ADD>{}, vec);
+        else f(integral_constant<int, Q8_F32>{}, vec);
+    };
+    if ((p.N & 3) == 0) with(integral_constant<bool, true>{});
+    else with(integral_constant<bool, false>{});
 }
 
 // A wave-uniform address, in scalar registers
@@ -94,15 +155,18 @@ template <class Op, int WM, int WN, int MB, int NB, int NS>
 __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int split, unsigned char *lds)
 {
     constexpr int NW = WM * WN, BM = 32 * MB * WM, BN = 32 * NB * WN;
-    constexpr int AI = BM / 8 / NW, BI = BN / 8 / NW, L = AI + BI;       // loads of a wavefront and stage
+    constexpr int AI = BM / 8 / NW, BI = BN / 8 / NW, L = AI + BI;     // loads of a wavefront and stage
     static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0, "every wavefront issues the same number of loads");
-    static_assert(NS >= 2 && NS <= 4 && (NS - 2) * L <= 63, "the wait counter has six bits");
+    static_assert(NS >= 2 && (NS - 1) * L <= 63, "the wait counter has six bits");
     constexpr int STAGE = (BM + BN) * 128;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int li = lane & 31, lh = lane >> 5;
     const int wm0 = (wave / WN) * 32 * MB, wn0 = (wave % WN) * 32 * NB;
-    const int tm = tile / p.tiles_n, tn = tile - tm * p.tiles_n;
+    // tiles run down groups of 8 tile rows: the ones that are computed at a time then share rows and columns (of 1024 tiles of 256 x 256, an
+    // XCD's 32 at a time read 12 tiles of operands from beyond its L2, row by row they would read 33)
+    const int tiles_m = (p.M + BM - 1) / BM, first = tile / (8 * p.tiles_n) * 8, high = min(8, tiles_m - first);
+    const int in_group = tile - first * p.tiles_n, tm = first + in_group % high, tn = in_group / high;
     const int m0 = tm * BM, n0 = tn * BN;
     const int ks_beg = split * p.ksteps_per_split;
     const int nst = min(p.ksteps, ks_beg + p.ksteps_per_split) - ks_beg;
@@ -127,17 +191,22 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
         asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
     };
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * 1024;
-    auto issue = [&](int ks, int buf) __attribute__((always_inline)) {
-        ks = __builtin_amdgcn_readfirstlane(ks);
-        const unsigned char *ap = ag + (size_t)ks * 128, *bp = bg + (size_t)(p.planes == 2 ? ks >> 1 : ks) * 128;
-        const unsigned da = lds0 + buf * STAGE, db = da + BM * 128;
-#pragma unroll
-        for (int i = 0; i < AI; i++) dma16(asrc[i], ap, da + NW * i * 1024);
-#pragma unroll
-        for (int i = 0; i < BI; i++) dma16(bsrc[i], bp, db + NW * i * 1024);
+    // the loads of step `ks` (past the last one: that again) into buffer `buf`: where from, and the i-th of them
+    const unsigned char *ap, *bp;
+    unsigned to;
+    const int ks_end = ks_beg + nst - 1;
+    auto aim = [&](int ks, int buf) __attribute__((always_inline)) {
+        ks = __builtin_amdgcn_readfirstlane(min(ks, ks_end));
+        ap = ag + (size_t)ks * 128;
+        bp = bg + (size_t)(p.planes == 2 ? ks >> 1 : ks) * 128;
+        to = lds0 + buf * STAGE;
+    };
+    auto load = [&](int i) __attribute__((always_inline)) {
+        if (i < AI) dma16(asrc[i < AI ? i : 0], ap, to + NW * i * 1024);
+        else dma16(bsrc[i < AI ? 0 : i - AI], bp, to + BM * 128 + NW * (i - AI) * 1024);
     };
 
-    unsigned fr[4];                                 // this lane's piece of a fragment's row, for each quarter of a step
+    unsigned fr[4];                                 // this lane's piece of a fragment's row, for each slice of 32 bytes
 #pragma unroll
     for (int kc = 0; kc < 4; kc++) fr[kc] = li * 128 + 16 * ((2 * kc + lh) ^ ((li >> 1) & 7));
 
@@ -149,59 +218,123 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
 #pragma unroll
             for (int r = 0; r < 16; r++) acc[i][j][r] = 0;
 
-    auto compute = [&](const unsigned char *sa, const unsigned char *sb) __attribute__((always_inline)) {
+    // A slice: its products, and between them the reads of the next slice's fragments (slice kc of buffer `buf`) and, in a stage's last
+    // one, the loads of another stage.  The order is kept as written: the compiler would gather the reads in front of
+    // the products that wait for them.
+    q8_i32x4 af[2][MB], bf[2][NB];
+    auto read1 = [&](int f, int kc, int buf, int side) __attribute__((always_inline)) {
+        const unsigned char *at = lds + buf * STAGE + fr[kc];
+        if (f < MB) af[side][f < MB ? f : 0] = *(const q8_i32x4 *)(at + (wm0 + 32 * f) * 128);
+        else bf[side][f < MB ? 0 : f - MB] = *(const q8_i32x4 *)(at + (BM + wn0 + 32 * (f - MB)) * 128);
+    };
+    auto slice = [&](int side, bool reads, int kc, int buf, bool loads) __attribute__((always_inline)) {
+        constexpr int P = MB * NB, F = MB + NB;
 #pragma unroll
-        for (int kc = 0; kc < 4; kc++) {
-            q8_i32x4 af[MB], bf[NB];
+        for (int t = 0; t < P; t++) {
+            if (reads)
 #pragma unroll
-            for (int i = 0; i < MB; i++) af[i] = *(const q8_i32x4 *)(sa + fr[kc] + (wm0 + 32 * i) * 128);
+                for (int f = 0; f < F; f++)
+                    if (f * P / F == t) read1(f, kc, buf, side ^ 1);
+            acc[t / NB][t % NB] = Op::mul(bf[side][t % NB], af[side][t / NB], acc[t / NB][t % NB]);
+            if (loads)
 #pragma unroll
-            for (int j = 0; j < NB; j++) bf[j] = *(const q8_i32x4 *)(sb + fr[kc] + (wn0 + 32 * j) * 128);
-#pragma unroll
-            for (int i = 0; i < MB; i++)
-#pragma unroll
-                for (int j = 0; j < NB; j++) acc[i][j] = Op::mul(af[i], bf[j], acc[i][j]);
+                for (int i = 0; i < L; i++)
+                    if (i * P / L == t) load(i);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
-    // s_waitcnt vmcnt(k stages' loads) lgkmcnt(0), expcnt untouched
+    // s_waitcnt vmcnt(k stages' loads) lgkmcnt(0), expcnt untouched; then the same of all wavefronts
 #define OWT_WAIT_STAGES(k) __builtin_amdgcn_s_waitcnt((((k) * L) & 15) | ((((k) * L) >> 4) << 14) | (7 << 4))
+    if (nst > 0) {
 #pragma unroll
-    for (int i = 0; i < NS - 1; i++)
-        if (i < nst) issue(ks_beg + i, i);
-    int cur = 0, fill = NS - 1;                     // stage s lives in buffer s % NS; `fill` is the buffer of stage s + NS - 1
-    for (int s = 0; s < nst; s++) {
-        // this wavefront's pieces of stage s have landed and its reads of stage s - 1 are done; behind the barrier that holds for all
-        const int ahead = min(NS - 2, nst - 1 - s);
-        if (ahead == 0) OWT_WAIT_STAGES(0);
-        else if (ahead == 1) OWT_WAIT_STAGES(1);
-        else OWT_WAIT_STAGES(NS >= 4 ? 2 : 1);
+        for (int s = 0; s < NS; s++) {
+            aim(ks_beg + s, s);
+#pragma unroll
+            for (int i = 0; i < L; i++) load(i);
+        }
+        OWT_WAIT_STAGES(NS - 1);
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        if (s + NS - 1 < nst) issue(ks_beg + s + NS - 1, fill);
-        compute(lds + cur * STAGE, lds + cur * STAGE + BM * 128);
-        cur = cur == NS - 1 ? 0 : cur + 1;
-        fill = fill == NS - 1 ? 0 : fill + 1;
+#pragma unroll
+        for (int f = 0; f < MB + NB; f++) read1(f, 0, 0, 0);
+        int cur = 0;                                // stage s lives in buffer s % NS
+        for (int s = 0; s < nst - 1; s++) {
+            const int next = cur == NS - 1 ? 0 : cur + 1;
+#pragma unroll
+            for (int kc = 0; kc < 3; kc++) slice(kc & 1, true, kc + 1, cur, false);
+            // stage s + 1 has landed and everybody has this stage's last fragments: its buffer is filled anew
+            asm volatile("" ::: "memory");
+            OWT_WAIT_STAGES(NS - 2);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            aim(ks_beg + s + NS, cur);
+            slice(1, true, 0, next, true);
+            cur = next;
+        }
+#pragma unroll
+        for (int kc = 0; kc < 3; kc++) slice(kc & 1, true, kc + 1, cur, false);
+        slice(1, false, 0, 0, false);
+        __builtin_amdgcn_s_waitcnt(0x0F70);         // vmcnt(0): the last loads into LDS have landed, too
     }
 #undef OWT_WAIT_STAGES
 
-    // accumulator register r of lane (li, lh): row 8 (r / 4) + 4 lh + r % 4, column li of its block
+    // Accumulator register r of lane (li, lh): column 8 (r / 4) + 4 lh + r % 4 of C, row li of its block (the operands change places in the
+    // instruction): four neighbouring results a lane.  They go through LDS, 32 rows of a wavefront at a time, so that rows are written as
+    // runs of 32 NB values; 16-byte piece q of row r sits in slot q ^ (r % 16) (or % 8).  The rows' scales come from LDS, too: a scale read
+    // from memory would wait for the stores before it.  One loop for each way of writing, not unrolled into one another: code that runs once
+    // a tile costs what its instructions take to arrive.
+    typedef decltype(typename Op::Acc()[0] + 0) S;
+    constexpr int QW = 8 * NB, SW = QW < 16 ? QW - 1 : 15;              // pieces of a row, and the bits of its swizzle
+    static_assert(NS * STAGE >= NW * 32 * QW * 16 + BM * 4, "32 rows of each wavefront and the rows' scales fit the stages");
+    unsigned char *mine = lds + wave * (32 * QW * 16);
+    int *rows = (int *)(lds + NW * (32 * QW * 16));
+    const int q = lane % QW, c = n0 + wn0 + 4 * q;
+    const Q8Cols k = q8_cols(p, c, typename Op::Acc());
+    __syncthreads();                                // everybody has read the last stage
+    for (int i = tid; i < BM; i += 64 * NW) rows[i] = q8_row(p, m0 + i, typename Op::Acc());
+    __syncthreads();
+    const int m_end = p.M - m0 - wm0;               // rows of this wavefront that exist
+    Q8GemmParams o = p;
+    if (p.splits > 1) o.out = (float *)p.partial + (size_t)split * p.M * p.N;
 #pragma unroll
-    for (int i = 0; i < MB; i++)
+    for (int i = 0; i < MB; i++) {
 #pragma unroll
-        for (int r = 0; r < 16; r++) {
-            const int row = m0 + wm0 + 32 * i + 8 * (r / 4) + 4 * lh + r % 4;
-            if (row >= p.M) continue;
+        for (int j = 0; j < NB; j++)
 #pragma unroll
-            for (int j = 0; j < NB; j++) {
-                const int col = n0 + wn0 + 32 * j + li;
-                if (col >= p.N) continue;
-                if (p.splits > 1) {
-                    auto *out = (decltype(acc[0][0][0] + 0) *)p.partial;
-                    out[((size_t)split * p.M + row) * p.N + col] = acc[i][j][r];
-                } else q8_finish(p, row, col, acc[i][j][r]);
+            for (int g = 0; g < 4; g++) {
+                q8_i32x4 v;
+#pragma unroll
+                for (int t = 0; t < 4; t++) {
+                    const S u = acc[i][j][4 * g + t];       // (a bit cast of the element in place takes the vector's first)
+                    v[t] = __builtin_bit_cast(int, u);
+                }
+                *(q8_i32x4 *)(mine + (li * QW + ((8 * j + 2 * g + lh) ^ (li & SW))) * 16) = v;
             }
-        }
+        q8_how(o, p.splits > 1, [&](auto how, auto vec) __attribute__((always_inline)) {
+            constexpr int HOW = decltype(how)::value;
+#pragma unroll 4
+            for (int it = 0; it < QW / 2; it++) {
+                const int r = it * (64 / QW) + lane / QW, at = 32 * i + r;
+                const q8_i32x4 w = *(const q8_i32x4 *)(mine + (r * QW + (q ^ (r & SW))) * 16);
+                if (at >= m_end) continue;
+                float v[4];
+                if (HOW == Q8_PARTIAL) {            // 32 bits each, as they are
+#pragma unroll
+                    for (int t = 0; t < 4; t++) v[t] = __int_as_float(w[t]);
+                } else {
+                    S sum[4];
+#pragma unroll
+                    for (int t = 0; t < 4; t++) {
+                        const int u = w[t];
+                        sum[t] = __builtin_bit_cast(S, u);
+                    }
+                    q8_values(p, k, rows[wm0 + at], sum, v);
+                }
+                q8_put<HOW, decltype(vec)::value>(o, m0 + wm0 + at, c, v);
+            }
+        });
+    }
 }
 
 template <class Op, int WM, int WN, int MB, int NB, int NS, int OCC>
@@ -213,16 +346,31 @@ __global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_
     q8gemm_tile<Op, WM, WN, MB, NB, NS>(p, tile, split, lds);
 }
 
-// Adds up the parts of a split sum, in order.
-template <class S>
+// Adds up the parts of a split sum, in order: four columns a thread.
+template <class Op>
 __global__ void __launch_bounds__(256) q8_join_kernel(const Q8GemmParams p)
 {
-    const size_t n = (size_t)p.M * p.N, stride = (size_t)gridDim.x * 256;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
-        S s = 0;
-        for (int k = 0; k < p.splits; k++) s += ((const S *)p.partial)[(size_t)k * n + i];
-        q8_finish(p, (int)(i / p.N), (int)(i % p.N), s);
-    }
+    typedef decltype(typename Op::Acc()[0] + 0) S;
+    const unsigned quads = (unsigned)(p.N + 3) / 4;
+    const size_t n = (size_t)p.M * quads, stride = (size_t)gridDim.x * 256, whole = (size_t)p.M * p.N;
+    q8_how(p, false, [&](auto how, auto vec) __attribute__((always_inline)) {
+        constexpr bool VEC = decltype(vec)::value;
+        for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
+            const int m = (int)(i / quads), c = (int)(i % quads) * 4;
+            const float *part = (const float *)p.partial + (size_t)m * p.N;
+            S s[4] = {};
+#pragma unroll 4
+            for (int k = 0; k < p.splits; k++) {
+                float v[4];
+                q8_load4<VEC>(part + k * whole, c, p.N, v);
+#pragma unroll
+                for (int t = 0; t < 4; t++) s[t] += __builtin_bit_cast(S, v[t]);
+            }
+            float v[4];
+            q8_values(p, q8_cols(p, c, typename Op::Acc()), q8_row(p, m, typename Op::Acc()), s, v);
+            q8_put<decltype(how)::value, VEC>(p, m, c, v);
+        }
+    });
 }
 
 }  // namespace owt
