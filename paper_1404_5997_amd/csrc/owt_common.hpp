@@ -133,6 +133,7 @@ __device__ __forceinline__ bool owt_split_major_wg(int ntiles, int splits, int &
 // 16 bytes through a raw buffer descriptor: a byte offset outside [0, bytes) reads as zeros without touching
 // memory, so bounds need no branch, no exec masking and no zeroing of the destination.
 typedef unsigned int owt_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int owt_u32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t owt_make_rsrc(const void *base, unsigned bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)bytes, 0x00020000);

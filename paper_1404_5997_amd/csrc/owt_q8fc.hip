@@ -168,7 +168,7 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
     p.lda = p.ldb = pitch;
     p.M = d->N; p.N = ol; p.ksteps = (int)(pitch / 128); p.planes = 1;
     p.out = y; p.bf16 = d->dtype == OWT_BF16;
-    p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, (d->flags & OWT_RELU) ? 1 : 0};
+    p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, (d->flags & OWT_RELU) ? 0.f : -INFINITY};
     return run_product<Q8Int>(p, pl, ws, (hipStream_t)hip_stream);
 }
 

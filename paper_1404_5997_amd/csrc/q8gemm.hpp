@@ -39,7 +39,7 @@ struct Q8Half {
 // Results of the forward pass: both scales, bias, ReLU, storage type
 struct Q8FwdOut {
     const float *xs, *ws, *bias;        // bias may be null
-    int relu;
+    float least;                        // 0 with ReLU, else minus infinity
 };
 // Results of a backward product: row m was scaled by 2^exps[m]
 struct Q8BwdOut {
@@ -104,7 +104,7 @@ __device__ __forceinline__ void q8_values(const Q8GemmParams &p, const Q8Cols &k
 #pragma unroll
     for (int t = 0; t < 4; t++) {
         v[t] = (float)sum[t] * (__int_as_float(row) * k.ws[t]) + k.bias[t];
-        if (p.f.relu) v[t] = v[t] < 0.f ? 0.f : v[t];           // (NaN stays)
+        v[t] = __builtin_elementwise_maximum(v[t], p.f.least);  // (NaN stays)
     }
 }
 __device__ __forceinline__ void q8_values(const Q8GemmParams &p, const Q8Cols &, int row, const float (&sum)[4], float (&v)[4])
@@ -112,20 +112,19 @@ __device__ __forceinline__ void q8_values(const Q8GemmParams &p, const Q8Cols &,
 #pragma unroll
     for (int t = 0; t < 4; t++) v[t] = ldexpf(sum[t], -row) * p.d.alpha;
 }
-// How results are written
+// How results are written: at row + c
 enum { Q8_PARTIAL, Q8_F32, Q8_F32_ADD, Q8_BF16 };
-template <int HOW, bool VEC> __device__ __forceinline__ void q8_put(const Q8GemmParams &p, int m, int c, float (&v)[4])
+template <int HOW, bool VEC> __device__ __forceinline__ void q8_put(const Q8GemmParams &p, void *row, int c, float (&v)[4])
 {
-    if (HOW == Q8_BF16) q8_store4<VEC>((bf16_t *)p.out + (size_t)m * p.N, c, p.N, v);
+    if (HOW == Q8_BF16) q8_store4<VEC>((bf16_t *)row, c, p.N, v);
     else {
-        float *row = (float *)p.out + (size_t)m * p.N;
         if (HOW == Q8_F32_ADD) {
             float old[4];
-            q8_load4<VEC>(row, c, p.N, old);
+            q8_load4<VEC>((float *)row, c, p.N, old);
 #pragma unroll
             for (int t = 0; t < 4; t++) v[t] += p.d.beta * old[t];
         }
-        q8_store4<VEC>(row, c, p.N, v);
+        q8_store4<VEC>((float *)row, c, p.N, v);
     }
 }
 // calls f(how, vec) with the constants of this product
@@ -259,11 +258,13 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
 #pragma unroll
         for (int f = 0; f < MB + NB; f++) read1(f, 0, 0, 0);
         int cur = 0;                                // stage s lives in buffer s % NS
-        for (int s = 0; s < nst - 1; s++) {
+        for (int s = 0; s < nst; s++) {
             const int next = cur == NS - 1 ? 0 : cur + 1;
 #pragma unroll
             for (int kc = 0; kc < 3; kc++) slice(kc & 1, true, kc + 1, cur, false);
-            // stage s + 1 has landed and everybody has this stage's last fragments: its buffer is filled anew
+            // Stage s + 1 has landed and everybody has this stage's last fragments: its buffer is filled anew.  (The last stages load the last
+            // step again, and the very last reads fragments of it that nothing uses: a second copy of this code would take longer to arrive
+            // than that does.)
             asm volatile("" ::: "memory");
             OWT_WAIT_STAGES(NS - 2);
             __builtin_amdgcn_s_barrier();
@@ -272,9 +273,6 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
             slice(1, true, 0, next, true);
             cur = next;
         }
-#pragma unroll
-        for (int kc = 0; kc < 3; kc++) slice(kc & 1, true, kc + 1, cur, false);
-        slice(1, false, 0, 0, false);
         __builtin_amdgcn_s_waitcnt(0x0F70);         // vmcnt(0): the last loads into LDS have landed, too
     }
 #undef OWT_WAIT_STAGES
@@ -282,8 +280,8 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     // Accumulator register r of lane (li, lh): column 8 (r / 4) + 4 lh + r % 4 of C, row li of its block (the operands change places in the
     // instruction): four neighbouring results a lane.  They go through LDS, 32 rows of a wavefront at a time, so that rows are written as
     // runs of 32 NB values; 16-byte piece q of row r sits in slot q ^ (r % 16) (or % 8).  The rows' scales come from LDS, too: a scale read
-    // from memory would wait for the stores before it.  One loop for each way of writing, not unrolled into one another: code that runs once
-    // a tile costs what its instructions take to arrive.
+    // from memory would wait for the stores before it.  A wavefront has its SIMD to itself here and an instruction
+    // takes it 8 clocks, so they are few: no branch, no 64-bit address (the first form took 30000 clocks of the end of a 256 x 256 tile).
     typedef decltype(typename Op::Acc()[0] + 0) S;
     constexpr int QW = 8 * NB, SW = QW < 16 ? QW - 1 : 15;              // pieces of a row, and the bits of its swizzle
     static_assert(NS * STAGE >= NW * 32 * QW * 16 + BM * 4, "32 rows of each wavefront and the rows' scales fit the stages");
@@ -294,9 +292,11 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     __syncthreads();                                // everybody has read the last stage
     for (int i = tid; i < BM; i += 64 * NW) rows[i] = q8_row(p, m0 + i, typename Op::Acc());
     __syncthreads();
-    const int m_end = p.M - m0 - wm0;               // rows of this wavefront that exist
-    Q8GemmParams o = p;
-    if (p.splits > 1) o.out = (float *)p.partial + (size_t)split * p.M * p.N;
+    const unsigned width = (unsigned)p.N * (p.splits == 1 && p.bf16 ? 2 : 4);       // (rows of up to 2^24 bytes: 128 of them are addressed with 32 bits)
+    unsigned char *base = (unsigned char *)q8_uniform((unsigned char *)(p.splits > 1 ? (char *)p.partial + (size_t)split * p.M * width : (char *)p.out) + (size_t)(m0 + wm0) * width);
+    const int m_end = __builtin_amdgcn_readfirstlane(max(0, min(32 * MB, p.M - m0 - wm0)));     // rows of this wavefront that exist
+    const unsigned char *src = mine + lane / QW * (QW * 16);
+    const int *factor = rows + wm0 + lane / QW;
 #pragma unroll
     for (int i = 0; i < MB; i++) {
 #pragma unroll
@@ -311,27 +311,52 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
                 }
                 *(q8_i32x4 *)(mine + (li * QW + ((8 * j + 2 * g + lh) ^ (li & SW))) * 16) = v;
             }
-        q8_how(o, p.splits > 1, [&](auto how, auto vec) __attribute__((always_inline)) {
+        q8_how(p, p.splits > 1, [&](auto how, auto vec) __attribute__((always_inline)) {
             constexpr int HOW = decltype(how)::value;
-#pragma unroll 4
-            for (int it = 0; it < QW / 2; it++) {
-                const int r = it * (64 / QW) + lane / QW, at = 32 * i + r;
-                const q8_i32x4 w = *(const q8_i32x4 *)(mine + (r * QW + (q ^ (r & SW))) * 16);
-                if (at >= m_end) continue;
-                float v[4];
-                if (HOW == Q8_PARTIAL) {            // 32 bits each, as they are
+            constexpr unsigned SIZE = HOW == Q8_BF16 ? 2 : 4;
+            // whole fours: through a descriptor that ends with the last row, where what lies outside is not written
+            const __amdgpu_buffer_rsrc_t rs = owt_make_rsrc(base, (unsigned)m_end * width);
+            unsigned at = c < p.N ? (unsigned)(32 * i + lane / QW) * width + (unsigned)c * SIZE : 0x80000000u;
+            const unsigned step = c < p.N ? (64 / QW) * width : 0;
+#pragma nounroll
+            for (int it = 0; it < QW / 2; it += 4) {        // four rows' reads at a time, then their results
+                q8_i32x4 w[4];
+                int f[4];
 #pragma unroll
-                    for (int t = 0; t < 4; t++) v[t] = __int_as_float(w[t]);
-                } else {
+                for (int u = 0; u < 4; u++) {
+                    const int r = (it + u) * (64 / QW);
+                    w[u] = *(const q8_i32x4 *)(src + r * (QW * 16) + (q ^ ((r + lane / QW) & SW)) * 16);
+                    f[u] = factor[32 * i + r];
+                }
+#pragma unroll
+                for (int u = 0; u < 4; u++) {
+                    float v[4];
                     S sum[4];
 #pragma unroll
                     for (int t = 0; t < 4; t++) {
-                        const int u = w[t];
-                        sum[t] = __builtin_bit_cast(S, u);
+                        const int e = w[u][t];
+                        sum[t] = __builtin_bit_cast(S, e);
+                        v[t] = __int_as_float(e);           // (a part of a sum: 32 bits as they are)
                     }
-                    q8_values(p, k, rows[wm0 + at], sum, v);
+                    if (HOW != Q8_PARTIAL) q8_values(p, k, f[u], sum, v);
+                    if (decltype(vec)::value) {
+                        if (HOW == Q8_F32_ADD) {
+                            const float4 old = buffer_load4(rs, at);
+                            v[0] += p.d.beta * old.x; v[1] += p.d.beta * old.y; v[2] += p.d.beta * old.z; v[3] += p.d.beta * old.w;
+                        }
+                        if (HOW == Q8_BF16) {
+                            const owt_u32x2 o = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+                            __builtin_amdgcn_raw_buffer_store_b64(o, rs, (int)at, 0, 0);
+                        } else {
+                            const owt_u32x4 o = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                            __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)at, 0, 0);
+                        }
+                        at += step;
+                    } else {
+                        const int m = 32 * i + (it + u) * (64 / QW) + lane / QW;
+                        if (m < m_end) q8_put<HOW, false>(p, base + (size_t)m * width, c, v);
+                    }
                 }
-                q8_put<HOW, decltype(vec)::value>(o, m0 + wm0 + at, c, v);
             }
         });
     }
@@ -368,7 +393,7 @@ __global__ void __launch_bounds__(256) q8_join_kernel(const Q8GemmParams p)
             }
             float v[4];
             q8_values(p, q8_cols(p, c, typename Op::Acc()), q8_row(p, m, typename Op::Acc()), s, v);
-            q8_put<decltype(how)::value, VEC>(p, m, c, v);
+            q8_put<decltype(how)::value, VEC>(p, (char *)p.out + (size_t)m * p.N * (p.bf16 ? 2 : 4), c, v);
         }
     });
 }
