@@ -104,11 +104,12 @@ struct Q8BwdLayout {
         nk = N > 0 ? (N + 63) / 64 : 1;
         ok = (O + 63) / 64;
         planes = bf16 ? 1 : 2;
-        // strips: enough parts of 64 columns for the chip, no more than 64 to add up
+        // strips: enough parts of 64 columns for the chip, no more than 64 to add up, and 64 rows or more each
         long want = (2048 + ok - 1) / ok;
         want = want > 64 ? 64 : want;
         long rows = (N + want - 1) / want;
-        rows = rows < 16 ? 16 : (rows + 3) / 4 * 4;
+        rows = (rows + 63) / 64 * 64;
+        rows = rows < 64 ? 64 : rows;
         strip_rows = (int)rows;
         strips = (int)((N + rows - 1) / rows);
         dw = q8_plan(O, I, 2 * nk);
@@ -196,25 +197,23 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     memset(&q, 0, sizeof(q));
     q.dy = dy; q.y = (d->flags & OWT_RELU) ? y_or_null : nullptr;
     q.xs = xscale; q.ws = wscale; q.xq = xq; q.wq = wq;
-    q.N = d->N; q.I = d->I; q.O = ol; q.bf16 = bf16; q.xpitch = q8_pitch(d->I);
-    q.want_dx = want_dx; q.dx_planes = l.planes;
+    q.N = d->N; q.I = d->I; q.O = ol; q.xpitch = q8_pitch(d->I);
+    q.want_dx = want_dx;
     q.alpha = alpha; q.beta = beta; q.db = dbias_or_null;
     q.strips = l.strips; q.strip_rows = l.strip_rows;
     q.colsum = (float *)(at + l.colsum); q.colmax = (float *)(at + l.colmax); q.rowmax = (float *)(at + l.rowmax);
     q.col_exp = (int *)(at + l.cexp); q.row_exp = (int *)(at + l.rexp);
     q.aw = (_Float16 *)(at + l.aw); q.ax = (_Float16 *)(at + l.ax); q.bw = (_Float16 *)(at + l.bw); q.bx = (_Float16 *)(at + l.bx);
     q.nk = l.nk; q.ok = l.ok;
-    const long its = (d->I + 63) / 64, tz = (long)l.nk * l.ok, tx = its * l.nk, tw = want_dx ? its * l.ok : 0;
-    if (tz + tx + tw > 0x7fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 tiles of 64 x 64 values");
-    q.tiles_z = (int)tz; q.tiles_x = (int)tx;
-    if (l.strips > 0) {
-        const dim3 grid((unsigned)l.ok, (unsigned)l.strips);
-        if (bf16) hipLaunchKernelGGL(q8_stat_kernel<bf16_t>, grid, dim3(256), 0, s, q);
-        else hipLaunchKernelGGL(q8_stat_kernel<float>, grid, dim3(256), 0, s, q);
-    }
-    const dim3 grid((unsigned)(tz + tx + tw));
-    if (bf16) hipLaunchKernelGGL(q8_prep_kernel<bf16_t>, grid, dim3(256), 0, s, q);
-    else hipLaunchKernelGGL(q8_prep_kernel<float>, grid, dim3(256), 0, s, q);
+    const long its = (d->I + 127) / 128, ts = (long)l.ok * l.strips, tx = its * l.nk, tw = want_dx ? its * l.ok : 0, tz = (long)l.nk * l.ok;
+    if (ts + tx + tw > 0x7fffffffL || tz > 0x7fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 tiles of 64 x 64 values");
+    q.tiles_s = (int)ts; q.tiles_x = (int)tx;
+    auto prepare = [&](auto stat, auto halves) {
+        hipLaunchKernelGGL(stat, dim3((unsigned)(ts + tx + tw)), dim3(256), 0, s, q);
+        hipLaunchKernelGGL(halves, dim3((unsigned)tz), dim3(256), 0, s, q);
+    };
+    if (bf16) { if (want_dx) prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, 1>); else prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, 0>); }
+    else { if (want_dx) prepare(q8_stat_kernel<float>, q8_prep_kernel<float, 2>); else prepare(q8_stat_kernel<float>, q8_prep_kernel<float, 0>); }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
 

@@ -6,10 +6,12 @@
 // values: that holds 22 bits of a value of 2^-16 of the row's largest and more, and 2^-39 of the largest below.  bf16 dx takes h alone (11
 // bits, where the result keeps 8).  A value that is not finite is h by itself.
 //
-// First launch: dz is read once for the bias gradient's sums and the largest magnitudes of columns (times xs) and rows (times ws), in
-// parts of 64 columns x a strip of rows.  Second launch: operands, 64 x 64 values a work-group, through LDS where they are transposed.
+// First launch: the whole numbers are turned, and dz is read once for the bias gradient's sums and the largest magnitudes of columns (times
+// xs) and rows (times ws), in parts of 64 columns x a strip of rows.  Second launch: the left operands, 64 x 64 values a work-group, the
+// one of dw turned through LDS.  Both are bound by memory: 8192 x 4096 -> 4096 in bf16 moves 490 MB.
 #pragma once
 #include "owt_common.hpp"
+#include "q8piece.hpp"
 
 namespace owt {
 
@@ -17,9 +19,9 @@ struct Q8PrepParams {
     const void *dy, *y;                 // y: ReLU mask, may be null
     const float *xs, *ws;
     const signed char *xq, *wq;
-    int N, I, O, bf16;
+    int N, I, O;
     size_t xpitch;                      // of xq and wq
-    int want_dx, dx_planes;
+    int want_dx;
     float alpha, beta;
     float *db;                          // may be null
     // scratch
@@ -28,147 +30,230 @@ struct Q8PrepParams {
     float *colmax;                      // [strips][O]
     float *rowmax;                      // [ceil(O/64)][N]
     int *col_exp, *row_exp;             // [O], [N]
-    _Float16 *aw, *ax, *bw, *bx;        // dw: [O][Nk][2][64], dx: [N][Ok][planes][64]; [I][Nk][64], [I][Ok][64] (Nk, Ok steps of 64)
+    _Float16 *aw, *ax, *bw, *bx;        // dw: [O][nk][2][64], dx: [N][ok][planes][64]; [I][nk][64], [I][ok][64]
     int nk, ok;                         // steps of 64 rows (tokens), of 64 outputs
-    int tiles_z, tiles_x;               // work-groups of the second launch: dz's, then xq's, then wq's
+    int tiles_s, tiles_x;               // work-groups of the first launch: statistics, then xq's tiles, then wq's
 };
 
-constexpr int kQ8PrepTile = 64;
-
-template <class T> __device__ __forceinline__ float q8_dz(const Q8PrepParams &p, size_t at)
+// dz of piece j of row n (zeros past the end of either)
+template <class T> __device__ __forceinline__ void q8_dz(const Q8PrepParams &p, int n, int j, float (&v)[Piece<T>::V])
 {
-    const float v = load1((const T *)p.dy + at, 0);
-    return p.y && !(load1((const T *)p.y + at, 0) > 0.f) ? 0.f : v;
+    constexpr int V = Piece<T>::V;
+    if (n >= p.N) {
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = 0.f;
+        return;
+    }
+    load_piece<T>((const T *)p.dy + (size_t)n * p.O, j, p.O, v);
+    if (p.y) {
+        float y[V];
+        load_piece<T>((const T *)p.y + (size_t)n * p.O, j, p.O, y);
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = y[i] > 0.f ? v[i] : 0.f;
+    }
 }
 // what a value adds to a largest finite magnitude
 __device__ __forceinline__ float q8_finite_abs(float v) { return fabsf(v) < __uint_as_float(0x7f800000u) ? fabsf(v) : 0.f; }
 // the power of two that takes it to [2^14, 2^15)
 __device__ __forceinline__ int q8_exponent(float largest) { return largest > 0.f ? 14 - ilogbf(largest) : 0; }
-
-// 256 threads: thread (c, r) = column c of 64, every fourth row of the strip.
-template <class T> __global__ void __launch_bounds__(256) q8_stat_kernel(const Q8PrepParams p)
-{
-    __shared__ float red[2][4][64];
-    const int c = threadIdx.x & 63, r = threadIdx.x >> 6, cb = blockIdx.x, strip = blockIdx.y, o = cb * 64 + c;
-    const int n_end = min(p.N, (strip + 1) * p.strip_rows);
-    const float ws = o < p.O ? p.ws[o] : 0.f;
-    float sum = 0.f, cmax = 0.f;
-    for (int n = strip * p.strip_rows + r; n < n_end; n += 4) {       // (a wavefront is one row of 64 columns: the loop is uniform in it)
-        const float dz = o < p.O ? q8_dz<T>(p, (size_t)n * p.O + o) : 0.f;
-        sum += dz;
-        cmax = fmaxf(cmax, q8_finite_abs(dz * p.xs[n]));
-        if (p.want_dx) {
-            float v = q8_finite_abs(dz * ws);
-#pragma unroll
-            for (int d = 32; d >= 1; d >>= 1) v = fmaxf(v, __shfl_xor(v, d, 64));
-            if (c == 0) p.rowmax[(size_t)cb * p.N + n] = v;
-        }
-    }
-    red[0][r][c] = sum;
-    red[1][r][c] = cmax;
-    __syncthreads();
-    if (r == 0 && o < p.O) {
-        p.colsum[(size_t)strip * p.O + o] = (red[0][0][c] + red[0][1][c]) + (red[0][2][c] + red[0][3][c]);
-        p.colmax[(size_t)strip * p.O + o] = fmaxf(fmaxf(red[1][0][c], red[1][1][c]), fmaxf(red[1][2][c], red[1][3][c]));
-    }
-}
-
-__device__ __forceinline__ void q8_halves(float v, int e, _Float16 &h, _Float16 &m)
+// v 2^e as two f16 values, the first in the low half
+__device__ __forceinline__ uint32_t q8_halves(float v, int e)
 {
     const float t = ldexpf(v, e);
-    h = (_Float16)t;
-    m = fabsf(t) < __uint_as_float(0x7f800000u) ? (_Float16)(t - (float)h) : (_Float16)0.f;
+    const _Float16 h = (_Float16)t, m = fabsf(t) < __uint_as_float(0x7f800000u) ? (_Float16)(t - (float)h) : (_Float16)0.f;
+    return (uint32_t)__builtin_bit_cast(uint16_t, h) | ((uint32_t)__builtin_bit_cast(uint16_t, m) << 16);
 }
 
-// A 64 x 64 tile of whole numbers q[k][i], as f16 to b[i][k]
-__device__ __forceinline__ void q8_turn(const signed char *q, size_t pitch, int K, int I, int kt, int it, _Float16 *b, int ksteps, unsigned char *lds)
+// The first launch's statistics: 64 columns of a strip of rows.  A wavefront reads 64 / LPR rows at a time, LPR lanes a row.
+template <class T> __device__ __forceinline__ void q8_stat(const Q8PrepParams &p, int cb, int strip, float *lds)
 {
-    // threads 16 a row of 4 values; LDS [k][i], rows of 68 bytes
-    const int tid = threadIdx.x;
+    constexpr int V = Piece<T>::V, LPR = 64 / V, RPW = 64 / LPR, AT = 4;      // AT pieces of a thread on their way at a time
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lc = lane % LPR, lr = lane / LPR, j = cb * LPR + lc;
+    const int n_end = min(p.N, (strip + 1) * p.strip_rows);
+    float ws[V], sum[V], cmax[V];
 #pragma unroll
-    for (int s = 0; s < 4; s++) {
-        const int k = s * 16 + (tid >> 4), i = (tid & 15) * 4;
-        // (a row is whole multiples of 128 bytes, so the four are inside it)
-        const uint32_t w = kt * 64 + k < K ? *(const uint32_t *)(q + (size_t)(kt * 64 + k) * pitch + it * 64 + i) : 0u;
-        *(uint32_t *)(lds + k * 68 + i) = w;
+    for (int i = 0; i < V; i++) {
+        ws[i] = j * V + i < p.O ? p.ws[j * V + i] : 0.f;
+        sum[i] = cmax[i] = 0.f;
+    }
+    for (int n0 = strip * p.strip_rows + wave * RPW * AT; n0 < n_end; n0 += 4 * RPW * AT) {
+        float dz[AT][V], xs[AT];
+#pragma unroll
+        for (int a = 0; a < AT; a++) {
+            const int n = n0 + a * RPW + lr;
+            xs[a] = n < n_end ? p.xs[n] : 0.f;
+            q8_dz<T>(p, n < n_end ? n : p.N, j, dz[a]);
+        }
+#pragma unroll
+        for (int a = 0; a < AT; a++) {
+            float r = 0.f;
+#pragma unroll
+            for (int i = 0; i < V; i++) {
+                sum[i] += dz[a][i];
+                cmax[i] = fmaxf(cmax[i], q8_finite_abs(dz[a][i] * xs[a]));
+                r = fmaxf(r, q8_finite_abs(dz[a][i] * ws[i]));
+            }
+            if (p.want_dx) {
+#pragma unroll
+                for (int d = LPR / 2; d >= 1; d >>= 1) r = fmaxf(r, __shfl_xor(r, d, 64));
+                const int n = n0 + a * RPW + lr;
+                if (lc == 0 && n < n_end) p.rowmax[(size_t)cb * p.N + n] = r;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) {
+#pragma unroll
+        for (int d = LPR; d < 64; d <<= 1) {
+            sum[i] += __shfl_xor(sum[i], d, 64);
+            cmax[i] = fmaxf(cmax[i], __shfl_xor(cmax[i], d, 64));
+        }
+        if (lr == 0) {
+            lds[wave * 64 + lc * V + i] = sum[i];
+            lds[256 + wave * 64 + lc * V + i] = cmax[i];
+        }
     }
     __syncthreads();
-    // threads 8 a row of 8 values
-#pragma unroll
-    for (int s = 0; s < 2; s++) {
-        const int i = s * 32 + (tid >> 3), k = (tid & 7) * 8;
-        if (it * 64 + i >= I) continue;
-        union { _Float16 h[8]; uint4 u; } v;
-#pragma unroll
-        for (int j = 0; j < 8; j++) v.h[j] = (_Float16)(float)(signed char)lds[(k + j) * 68 + i];
-        *(uint4 *)(b + ((size_t)(it * 64 + i) * ksteps + kt) * 64 + k) = v.u;
+    const int c = threadIdx.x, o = cb * 64 + c;
+    if (c < 64 && o < p.O) {
+        p.colsum[(size_t)strip * p.O + o] = (lds[c] + lds[64 + c]) + (lds[128 + c] + lds[192 + c]);
+        p.colmax[(size_t)strip * p.O + o] = fmaxf(fmaxf(lds[256 + c], lds[320 + c]), fmaxf(lds[384 + c], lds[448 + c]));
     }
 }
 
-template <class T> __global__ void __launch_bounds__(256) q8_prep_kernel(const Q8PrepParams p)
+// Whole numbers q[k][i], 64 k x 128 i, as f16 to b[i][k].  The rows are whole multiples of 128 bytes, so a tile's 128 are inside them.
+typedef _Float16 q8_f16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ void q8_turn(const signed char *q, size_t pitch, int K, int I, int kt, int it, _Float16 *b, int ksteps, unsigned *lds)
 {
-    __shared__ __attribute__((aligned(16))) float tile[64 * 65];
-    __shared__ int ce[64], re[64];
+    constexpr int P = 33;                           // words of a row in LDS: the eight rows and eight words that lanes read lie in 64 banks
     const int tid = threadIdx.x;
-    int b = blockIdx.x;
-    if (b >= p.tiles_z) {
-        b -= p.tiles_z;
-        const int its = (p.I + 63) / 64;
-        if (b < p.tiles_x) q8_turn(p.xq, p.xpitch, p.N, p.I, b / its, b % its, p.bw, p.nk, (unsigned char *)tile);
-        else {
-            b -= p.tiles_x;
-            q8_turn(p.wq, p.xpitch, p.O, p.I, b / its, b % its, p.bx, p.ok, (unsigned char *)tile);
-        }
-        return;
+    uint4 w[2];
+#pragma unroll
+    for (int s = 0; s < 2; s++) {
+        const int k = s * 32 + (tid >> 3);
+        w[s] = kt * 64 + k < K ? *(const uint4 *)(q + (size_t)(kt * 64 + k) * pitch + it * 128 + (tid & 7) * 16) : make_uint4(0, 0, 0, 0);
     }
-    const int nt = b / p.ok, ot = b % p.ok, n0 = nt * 64, o0 = ot * 64;
+#pragma unroll
+    for (int s = 0; s < 2; s++) {
+        unsigned *at = lds + (s * 32 + (tid >> 3)) * P + (tid & 7) * 4;
+        at[0] = w[s].x; at[1] = w[s].y; at[2] = w[s].z; at[3] = w[s].w;
+    }
+    __syncthreads();
+    const int ko = tid & 7, i4 = tid >> 3;          // eight k, four i
+    unsigned r[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) r[j] = lds[(ko * 8 + j) * P + i4] ^ 0x80808080u;        // 128 added to each
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+        const int i = it * 128 + i4 * 4 + t;
+        unsigned h[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            // 0x64uu is 1024 + uu in f16
+            const unsigned two = __builtin_amdgcn_perm(r[2 * j + 1], r[2 * j], 0x0c000c00u | (unsigned)t | ((unsigned)(4 + t) << 16)) | 0x64006400u;
+            const q8_f16x2 v = __builtin_bit_cast(q8_f16x2, two) - (q8_f16x2){1152.f, 1152.f};
+            h[j] = __builtin_bit_cast(unsigned, v);
+        }
+        if (i < I) *(uint4 *)(b + ((size_t)i * ksteps + kt) * 64 + ko * 8) = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+}
+
+template <class T> __global__ void __launch_bounds__(256) q8_stat_kernel(const Q8PrepParams p)
+{
+    __shared__ __attribute__((aligned(16))) unsigned lds[64 * 33];
+    int b = blockIdx.x;
+    const int its = (p.I + 127) / 128;
+    if (b < p.tiles_s) q8_stat<T>(p, b % p.ok, b / p.ok, (float *)lds);
+    else if ((b -= p.tiles_s) < p.tiles_x) q8_turn(p.xq, p.xpitch, p.N, p.I, b / its, b % its, p.bw, p.nk, lds);
+    else {
+        b -= p.tiles_x;
+        q8_turn(p.wq, p.xpitch, p.O, p.I, b / its, b % its, p.bx, p.ok, lds);
+    }
+}
+
+template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel(const Q8PrepParams p)      // DX: planes of dx's operand, 0 = none
+{
+    constexpr int V = Piece<T>::V, LPR = 64 / V, RPP = 256 / LPR, PASSES = 64 / RPP;    // lanes a row, rows a pass
+    __shared__ uint32_t tile[64 * 65];              // [n][o], both halves of a value in a word
+    __shared__ int ce[64], re[64];
+    const int tid = threadIdx.x, nt = blockIdx.x / p.ok, ot = blockIdx.x % p.ok, n0 = nt * 64, o0 = ot * 64;
+    const int lc = tid % LPR, lr = tid / LPR;
+    float dz[PASSES][V], ws[V], xs[PASSES];
+#pragma unroll
+    for (int s = 0; s < PASSES; s++) {
+        const int n = n0 + s * RPP + lr;
+        q8_dz<T>(p, n, ot * LPR + lc, dz[s]);
+        xs[s] = n < p.N ? p.xs[n] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < V; i++) ws[i] = o0 + lc * V + i < p.O ? p.ws[o0 + lc * V + i] : 0.f;
     if (tid < 64) {                                 // exponents of the columns; the bias gradient
         const int o = o0 + tid;
         float mx = 0.f, s = 0.f;
-        if (o < p.O)
-            for (int k = 0; k < p.strips; k++) {
-                mx = fmaxf(mx, p.colmax[(size_t)k * p.O + o]);
-                if (nt == 0) s += p.colsum[(size_t)k * p.O + o];
-            }
+        if (o < p.O) {
+#pragma unroll 8
+            for (int k = 0; k < p.strips; k++) mx = fmaxf(mx, p.colmax[(size_t)k * p.O + o]);
+            if (nt == 0)
+#pragma unroll 8
+                for (int k = 0; k < p.strips; k++) s += p.colsum[(size_t)k * p.O + o];
+        }
         ce[tid] = q8_exponent(mx);
         if (nt == 0 && o < p.O) {
             p.col_exp[o] = ce[tid];
             if (p.db) p.db[o] = p.alpha * s + (p.beta != 0.f ? p.beta * p.db[o] : 0.f);
         }
-    } else if (tid < 128 && p.want_dx) {            // and of the rows
-        const int n = n0 + tid - 64, cbs = (p.O + 63) / 64;
+    } else if (tid < 128 && DX) {                   // and of the rows
+        const int n = n0 + tid - 64, cbs = p.ok;
         float mx = 0.f;
         if (n < p.N)
+#pragma unroll 8
             for (int k = 0; k < cbs; k++) mx = fmaxf(mx, p.rowmax[(size_t)k * p.N + n]);
         re[tid - 64] = q8_exponent(mx);
         if (ot == 0 && n < p.N) p.row_exp[n] = re[tid - 64];
     }
-    const int c = tid & 63, r = tid >> 6, o = o0 + c;
-    const float ws = o < p.O ? p.ws[o] : 0.f;
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 16; k++) {
-        const int n = n0 + 4 * k + r;
-        const float dz = n < p.N && o < p.O ? q8_dz<T>(p, (size_t)n * p.O + o) : 0.f;
-        tile[(4 * k + r) * 65 + c] = n < p.N ? dz * p.xs[n] : 0.f;
-        if (p.want_dx && n < p.N) {
-            _Float16 h, m;
-            q8_halves(dz * ws, re[4 * k + r], h, m);
-            _Float16 *at = p.ax + ((size_t)n * p.ok + ot) * p.dx_planes * 64 + c;
-            at[0] = h;
-            if (p.dx_planes == 2) at[64] = m;
+    for (int s = 0; s < PASSES; s++) {
+        const int r = s * RPP + lr, n = n0 + r;
+#pragma unroll
+        for (int i = 0; i < V; i++) tile[r * 65 + lc * V + i] = n < p.N ? q8_halves(dz[s][i] * xs[s], ce[lc * V + i]) : 0u;
+        if (DX && n < p.N) {
+            uint32_t both[V], h[V / 2], m[V / 2];
+            const int e = re[r];
+#pragma unroll
+            for (int i = 0; i < V; i++) both[i] = q8_halves(dz[s][i] * ws[i], e);
+#pragma unroll
+            for (int i = 0; i < V / 2; i++) {
+                h[i] = __builtin_amdgcn_perm(both[2 * i + 1], both[2 * i], 0x05040100u);
+                m[i] = __builtin_amdgcn_perm(both[2 * i + 1], both[2 * i], 0x07060302u);
+            }
+            _Float16 *at = p.ax + ((size_t)n * p.ok + ot) * (DX * 64) + lc * V;
+            if (V == 8) {
+                *(uint4 *)at = make_uint4(h[0], h[1], h[V / 2 - 2], h[V / 2 - 1]);
+                if (DX == 2) *(uint4 *)(at + 64) = make_uint4(m[0], m[1], m[V / 2 - 2], m[V / 2 - 1]);
+            } else {
+                *(uint2 *)at = make_uint2(h[0], h[1]);
+                if (DX == 2) *(uint2 *)(at + 64) = make_uint2(m[0], m[1]);
+            }
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < 16; k++) {                  // a wavefront writes a row of 64 tokens
-        const int oc = 4 * k + r;
+    for (int s = 0; s < 2; s++) {                   // eight tokens of an output a thread, eight threads a row of 64
+        const int oc = s * 32 + (tid >> 3), ko = tid & 7;
         if (o0 + oc >= p.O) continue;
-        _Float16 h, m;
-        q8_halves(tile[c * 65 + oc], ce[oc], h, m);
-        _Float16 *at = p.aw + ((size_t)(o0 + oc) * p.nk + nt) * 128 + c;
-        at[0] = h;
-        at[64] = m;
+        uint32_t both[8];
+#pragma unroll
+        for (int j = 0; j < 8; j++) both[j] = tile[(ko * 8 + j) * 65 + oc];
+        uint32_t h[4], m[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            h[j] = __builtin_amdgcn_perm(both[2 * j + 1], both[2 * j], 0x05040100u);
+            m[j] = __builtin_amdgcn_perm(both[2 * j + 1], both[2 * j], 0x07060302u);
+        }
+        _Float16 *at = p.aw + ((size_t)(o0 + oc) * p.nk + nt) * 128 + ko * 8;
+        *(uint4 *)at = make_uint4(h[0], h[1], h[2], h[3]);
+        *(uint4 *)(at + 64) = make_uint4(m[0], m[1], m[2], m[3]);
     }
 }
 
