@@ -337,7 +337,8 @@ const char *owt_last_error(void);
  * 71 its forward pass in one launch; bf16 of any channel counts:
  * 80..86 stride-1 filter gradient, 87..89 filter gradient of any geometry, 90 forward / backward-data and strided
  * forward, 92..94 forward / backward-data of layers of few tiles; 100..106 the bf16 filter gradient over images
- * that streams its operands into LDS; 110..112 the products of the dense shard in 8 bits), `splitk` > 0 forces the
+ * that streams its operands into LDS; 110..112 the products of the dense shard in 8 bits,
+ * 113 its forward product of few results), `splitk` > 0 forces the
  * split count of the reduction (clamped to the number of reduction steps), `flags` is a set of
  * OWT_FORCE_* bits.  While an override is active, tuned and cached plans are ignored.  The three
  * values are stored atomically, but a launch that runs concurrently with this call may see the old

@@ -101,9 +101,11 @@ def _ptr(t):
     """Device pointer of a torch tensor (or a raw int / None passed through)."""
     if t is None:
         return None
-    if isinstance(t, int):
+    try:
+        dense = t.is_contiguous()
+    except AttributeError:
         return t
-    if not t.is_contiguous():
+    if not dense:
         raise ValueError("owt takes dense row-major tensors")
     return t.data_ptr()
 

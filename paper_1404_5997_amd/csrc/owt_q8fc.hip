@@ -4,15 +4,19 @@
 
 #include "owt_host.hpp"
 #include "q8.hpp"
+#include "q8few.hpp"
 #include "q8gemm.hpp"
 #include "q8prep.hpp"
 
 namespace owt {
 
-struct Q8Tile { int bm, bn, occ; float step_us, start_us; };
-constexpr int kNumQ8Tiles = 3, kQ8FirstTile = 110;      // owt_test_force_variant: tile numbers 110.. name these
-// microseconds of a step of a work-group on a full chip, and of its start and end
-static const Q8Tile kQ8Tiles[kNumQ8Tiles] = {{256, 256, 1, 1.6f, 4.f}, {128, 128, 1, 0.6f, 2.5f}, {64, 64, 2, 0.5f, 2.f}};
+// Tiles of the products, 256 x 256, 128 x 128 and 64 x 64 (owt_test_force_variant: 110.. name these), and the forward product's kernel for
+// few results (113).
+constexpr int kNumQ8Tiles = 3, kQ8FirstTile = 110, kQ8Few = 3;
+// What a work-group takes: `start` for its beginning and end, `step` for a step on a quiet chip, `busy` where 128 or more run (256 x 256:
+// all 256; the chip is then bound by its power).  us, fitted to 20 products of 1 x 1024 -> 1024 to 8192 x 4096 -> 8192 with every tile and split.
+struct Q8Tile { int bm, bn; float start, step, busy; };
+static const Q8Tile kQ8Tiles[kNumQ8Tiles] = {{256, 256, 11.f, 1.05f, 1.5f}, {128, 128, 3.f, 0.4f, 0.55f}, {64, 64, 1.2f, 0.21f, 0.21f}};
 
 template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, hipStream_t s)
 {
@@ -24,23 +28,29 @@ template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, 
 }
 
 struct Q8Plan { int tile, splits; };
-static Q8Plan q8_plan(long M, long N, int ksteps)
+static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
 {
     Q8Plan best{0, 1};
     float least = 1e30f;
     const int want = forced_tile() - kQ8FirstTile, want_split = forced_split();
+    if (forward && want == kQ8Few) return {kQ8Few, 1};
     for (int t = 0; t < kNumQ8Tiles; t++) {
         if (want >= 0 && want < kNumQ8Tiles && t != want) continue;
         const Q8Tile &q = kQ8Tiles[t];
         const long tiles = ((M + q.bm - 1) / q.bm) * ((N + q.bn - 1) / q.bn);
         for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= ksteps && tiles * sp <= 1024)); sp *= 2) {
-            const long rounds = (tiles * sp + 256 * q.occ - 1) / (256 * q.occ);
-            float us = (float)rounds * ((float)((ksteps + sp - 1) / sp) * q.step_us + q.start_us);
-            if (sp > 1) us += 4.f + (float)(sp + 1) * (float)M * (float)N * 4e-6f / 4.f;
+            const long each = (tiles * sp + 255) / 256;         // work-groups of a CU
+            const float step = tiles * sp >= (t == 0 ? 256 : 128) ? q.busy : q.step;
+            float us = 3.f + (float)each * (q.start + (float)((ksteps + sp - 1) / sp) * step);
+            if (sp > 1) us += (N % 4 ? 5.6f : 3.6f) + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
             if (us < least) { least = us; best = {t, sp}; }
         }
     }
     if (want_split > 0) best.splits = want_split < ksteps ? want_split : ksteps;
+    else if (forward && want < 0) {     // 16 x 16 results a work-group: 1.5 us and 0.08 a step (16 rows of 4096 -> 4096 take 7.2 us, tiles 9.7)
+        const long tiles = ((M + 15) / 16) * ((N + 15) / 16);
+        if (3.f + (float)((tiles + 255) / 256) * (1.5f + 0.08f * (float)ksteps) < least) best = {kQ8Few, 1};
+    }
     return best;
 }
 
@@ -112,8 +122,8 @@ struct Q8BwdLayout {
         rows = rows < 64 ? 64 : rows;
         strip_rows = (int)rows;
         strips = (int)((N + rows - 1) / rows);
-        dw = q8_plan(O, I, 2 * nk);
-        dx = q8_plan(N, I, planes * ok);
+        dw = q8_plan(O, I, 2 * nk, false);
+        dx = q8_plan(N, I, planes * ok, false);
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
         colsum = take((size_t)strips * O * 4);
@@ -146,7 +156,7 @@ size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass)
     if (pass == OWT_PASS_FWD) {
         if (d->N == 0) return 0;
         const int ks = (int)(q8_pitch(d->I) / 128);
-        return partial_bytes(q8_plan(d->N, ol, ks), d->N, ol);
+        return partial_bytes(q8_plan(d->N, ol, ks, true), d->N, ol);
     }
     return Q8BwdLayout(d->N, d->I, ol, d->dtype == OWT_BF16).total;
 }
@@ -161,7 +171,7 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
     OWT_TRY(need_ptr(y, "y"));
     if (d->flags & OWT_BIAS) OWT_TRY(need_ptr(bias, "bias"));
     const size_t pitch = q8_pitch(d->I);
-    const Q8Plan pl = q8_plan(d->N, ol, (int)(pitch / 128));
+    const Q8Plan pl = q8_plan(d->N, ol, (int)(pitch / 128), true);
     OWT_TRY(need_ws(ws, ws_bytes, partial_bytes(pl, d->N, ol)));
     Q8GemmParams p;
     memset(&p, 0, sizeof(p));
@@ -170,6 +180,14 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
     p.M = d->N; p.N = ol; p.ksteps = (int)(pitch / 128); p.planes = 1;
     p.out = y; p.bf16 = d->dtype == OWT_BF16;
     p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, (d->flags & OWT_RELU) ? 0.f : -INFINITY};
+    if (pl.tile == kQ8Few) {
+        const long tiles = (long)((p.M + 15) / 16) * ((p.N + 15) / 16);
+        if (tiles > 0x3fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+        p.tiles = (int)tiles;
+        hipLaunchKernelGGL(q8_few_kernel, dim3((unsigned)owt_split_major_grid(p.tiles, 1)), dim3(1024), 0, (hipStream_t)hip_stream, p);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+    }
     return run_product<Q8Int>(p, pl, ws, (hipStream_t)hip_stream);
 }
 

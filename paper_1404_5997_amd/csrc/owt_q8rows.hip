@@ -38,13 +38,13 @@ template <class T> static void launch_unpack(const signed char *q, const float *
                        q8_pitch(cols), lpr, segs);
 }
 
-// Strips of rows that the backward pass sums the gain's gradient over, one in flight for each group of threads: 4 work-groups a CU are
-// enough to hide its loads, and more would only be more partial sums to write and read.
-static int bwd_strips(int rows, int cols, int tpr)
+// Strips of rows that the backward pass sums the gain's gradient over, one in flight for each group of threads: as many as hide its loads
+// (more would only be more partial sums to write and read), and few enough that all have the same number of rows, or one less.
+static int bwd_strips(int rows, int tpr)
 {
-    const int most = tpr >= 1024 ? 512 : tpr >= 256 ? 1024 : 256 * 4 * (256 / tpr);
-    (void)cols;
-    return rows < most ? rows : most;
+    const int most = tpr >= 1024 ? 256 : tpr >= 256 ? 1024 : 256 * 4 * (256 / tpr);
+    const int each = (rows + most - 1) / most;
+    return each > 0 ? (rows + each - 1) / each : 0;
 }
 struct BwdShape { int tpr, p; };
 static BwdShape bwd_shape(int cols, int v)
@@ -150,7 +150,7 @@ size_t owt_rmsnorm_q8_workspace_bytes(int rows, int cols)
     if (cols > kNormMaxCols) { fail(OWT_EUNSUPPORTED, "norm over more than %d values", kNormMaxCols); return (size_t)-1; }
     size_t most = 0;                    // of both storage types: a program may size its scratch before it knows
     for (int v : {4, 8}) {
-        const size_t n = (size_t)bwd_strips(rows, cols, bwd_shape(cols, v).tpr) * cols * sizeof(float);
+        const size_t n = (size_t)bwd_strips(rows, bwd_shape(cols, v).tpr) * cols * sizeof(float);
         most = n > most ? n : most;
     }
     return most;
@@ -166,7 +166,7 @@ owt_status owt_rmsnorm_q8_bwd(int rows, int cols, owt_dtype dtype, const void *d
     if (rows > 0) OWT_TRY(check_pointers({dy, h, rstd, dh}, {gain_or_null, dres_or_null}));
     OWT_TRY(check_pointers({}, {dgain_or_null}));
     const BwdShape f = bwd_shape(cols, dtype == OWT_F32 ? 4 : 8);
-    const int strips = bwd_strips(rows, cols, f.tpr);
+    const int strips = bwd_strips(rows, f.tpr);
     if (dgain_or_null) {
         const size_t need = (size_t)strips * cols * sizeof(float);
         if (ws_bytes < need) return fail(OWT_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws_bytes);

@@ -228,17 +228,24 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rmsnorm_bwd_kernel(cons
     if (TPR <= 64 && strip >= p.strips) return;     // (wider rows have a work-group to themselves and a strip each)
     const int full = (p.cols + V - 1) / V;
     const float inv = 1.f / (float)p.cols;
-    float gain[P][V], sum[P][V];
-#pragma unroll
-    for (int k = 0; k < P; k++)
+    // The gain stays in registers, too, where they hold it: not for more than 16 values of each of 1024 threads.
+    constexpr bool HELD = P * V <= 16 || TPR < 1024;
+    float gain[HELD ? P : 1][V], sum[P][V];
+    auto fetch_gain = [&](int k, float (&to)[V]) __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < V / 4; c++) {
             float g[4] = {1.f, 1.f, 1.f, 1.f};
-            const int j = (k * TPR + t0) * (V / 4) + c;
-            if (p.gain) load_piece<float>(p.gain, j, p.cols, g);
+            if (p.gain) load_piece<float>(p.gain, (k * TPR + t0) * (V / 4) + c, p.cols, g);
 #pragma unroll
-            for (int i = 0; i < 4; i++) { gain[k][4 * c + i] = g[i]; sum[k][4 * c + i] = 0.f; }
+            for (int i = 0; i < 4; i++) to[4 * c + i] = g[i];
         }
+    };
+#pragma unroll
+    for (int k = 0; k < P; k++) {
+        if (HELD) fetch_gain(k, gain[HELD ? k : 0]);
+#pragma unroll
+        for (int i = 0; i < V; i++) sum[k][i] = 0.f;
+    }
     int turn = 0;
     for (size_t row = strip; row < (size_t)p.rows; row += p.strips, turn ^= 1) {
         const size_t at = row * p.cols;
@@ -255,14 +262,16 @@ __global__ void __launch_bounds__(TPR > 256 ? TPR : 256) rmsnorm_bwd_kernel(cons
                 for (int i = 0; i < V; i++) h[k][i] = d[k][i] = 0.f;
         }
 #pragma unroll
-        for (int k = 0; k < P; k++)
+        for (int k = 0; k < P; k++) {
+            if (!HELD) fetch_gain(k, gain[0]);
 #pragma unroll
             for (int i = 0; i < V; i++) {
                 h[k][i] *= rstd;
                 sum[k][i] = fmaf(d[k][i], h[k][i], sum[k][i]);
-                d[k][i] *= gain[k][i];
+                d[k][i] *= gain[HELD ? k : 0][i];
                 dot = fmaf(d[k][i], h[k][i], dot);
             }
+        }
         uint32_t none = 0;
         row_reduce<TPR>(dot, none, red[turn], t0);
         const float mean = dot * inv;
@@ -303,6 +312,7 @@ __global__ void __launch_bounds__(256) rmsnorm_dgain_kernel(const float *__restr
     const int cl = threadIdx.x & 15, ph = threadIdx.x >> 4, c = blockIdx.x * 16 + cl;
     float s = 0.f;
     if (c < cols)
+#pragma unroll 16
         for (int k = ph; k < strips; k += 16) s += partial[(size_t)k * cols + c];
     red[ph][cl] = s;
     __syncthreads();

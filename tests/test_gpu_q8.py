@@ -335,6 +335,14 @@ def test_every_tile_and_split_of_the_products(tile, splits):
             Shard(N, I, O, "f32").check_backward()
 
 
+@pytest.mark.parametrize("N,I,O", [(1, 1, 1), (1, 4096, 130), (16, 2500, 32), (3, 13000, 20), (17, 9216, 33), (65, 129, 31), (300, 700, 260)])
+def test_the_forward_kernel_of_few_results(N, I, O):
+    say("case few", N, I, O)
+    with force(113):
+        Shard(N, I, O, "f32").check_forward()
+        Shard(N, I, O, "bf16", bias=False, relu=False).check_forward()
+
+
 def test_shard_of_the_largest_sums():
     """Every product 127 * 127 (and 128 * 128, which rows of one's own may hold): sums just short of 2^31, exact in whole numbers."""
     m = owt()
