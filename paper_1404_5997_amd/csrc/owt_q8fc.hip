@@ -27,13 +27,14 @@ template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, 
     return hipGetLastError();
 }
 
-struct Q8Plan { int tile, splits; };
+struct Q8Plan { int tile, splits; float us; };
 static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
 {
-    Q8Plan best{0, 1};
-    float least = 1e30f;
+    Q8Plan best{0, 1, 0.f};
+    float &least = best.us;
+    least = 1e30f;
     const int want = forced_tile() - kQ8FirstTile, want_split = forced_split();
-    if (forward && want == kQ8Few) return {kQ8Few, 1};
+    if (forward && want == kQ8Few) return {kQ8Few, 1, 0.f};
     for (int t = 0; t < kNumQ8Tiles; t++) {
         if (want >= 0 && want < kNumQ8Tiles && t != want) continue;
         const Q8Tile &q = kQ8Tiles[t];
@@ -43,28 +44,53 @@ static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
             const float step = tiles * sp >= (t == 0 ? 256 : 128) ? q.busy : q.step;
             float us = 3.f + (float)each * (q.start + (float)((ksteps + sp - 1) / sp) * step);
             if (sp > 1) us += (N % 4 ? 5.6f : 3.6f) + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
-            if (us < least) { least = us; best = {t, sp}; }
+            if (us < least) best = {t, sp, us};
         }
     }
     if (want_split > 0) best.splits = want_split < ksteps ? want_split : ksteps;
     else if (forward && want < 0) {     // 16 x 16 results a work-group: 1.5 us and 0.08 a step (16 rows of 4096 -> 4096 take 7.2 us, tiles 9.7)
         const long tiles = ((M + 15) / 16) * ((N + 15) / 16);
-        if (3.f + (float)((tiles + 255) / 256) * (1.5f + 0.08f * (float)ksteps) < least) best = {kQ8Few, 1};
+        if (3.f + (float)((tiles + 255) / 256) * (1.5f + 0.08f * (float)ksteps) < least) best = {kQ8Few, 1, 0.f};
+    }
+    return best;
+}
+
+// Both backward products in one launch of the same tile: the two tiles that have one.  0: apart they take less.
+static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long O, int dx_steps, int dw_steps)
+{
+    const int want = forced_tile() - kQ8FirstTile;
+    if (forced_split() > 0) return 0;
+    int best = 0;
+    float least = dx.us + dw.us;
+    for (int t = 1; t < kNumQ8Tiles; t++) {
+        if (want >= 0 && want < kNumQ8Tiles && t != want) continue;
+        const Q8Tile &q = kQ8Tiles[t];
+        const float tx = (float)(((N + q.bm - 1) / q.bm) * ((I + q.bn - 1) / q.bn)), tw = (float)(((O + q.bm - 1) / q.bm) * ((I + q.bn - 1) / q.bn));
+        const float ux = q.start + (float)dx_steps * q.busy, uw = q.start + (float)dw_steps * q.busy;
+        float us = (tx * ux + tw * uw) / 256.f + 0.5f * (ux > uw ? ux : uw);
+        us = 3.f + (us > ux ? us : ux);
+        if (us < least) { least = us; best = t; }
     }
     return best;
 }
 
 static size_t partial_bytes(const Q8Plan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
 
-template <class Op> static owt_status run_product(Q8GemmParams p, const Q8Plan &pl, void *partial, hipStream_t s)
+// Numbers the tiles of a product.
+static bool lay_tiles(Q8GemmParams &p, const Q8Plan &pl)
 {
     const Q8Tile &q = kQ8Tiles[pl.tile];
     p.tiles_n = (p.N + q.bn - 1) / q.bn;
     const long tiles = (long)p.tiles_n * ((p.M + q.bm - 1) / q.bm);
-    if (tiles * pl.splits > 0x3fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
     p.tiles = (int)tiles;
     p.splits = pl.splits;
     p.ksteps_per_split = ((p.ksteps / p.planes + pl.splits - 1) / pl.splits) * p.planes;
+    return tiles * pl.splits <= 0x3fffffffL;
+}
+
+template <class Op> static owt_status run_product(Q8GemmParams p, const Q8Plan &pl, void *partial, hipStream_t s)
+{
+    if (!lay_tiles(p, pl)) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
     p.partial = partial;
     hipError_t e = launch_tile<Op>(pl.tile, p, s);
     if (e == hipSuccess && pl.splits > 1) {
@@ -106,7 +132,7 @@ static owt_status need_ws(const void *ws, size_t have, size_t need)
 
 // The backward pass's scratch, laid out in order; `take` returns the offset of each part.
 struct Q8BwdLayout {
-    int nk, ok, strips, strip_rows, planes;
+    int nk, ok, strips, strip_rows, planes, pair;
     Q8Plan dw, dx;
     size_t colsum, colmax, rowmax, cexp, rexp, aw, ax, bw, bx, partial, total;
     Q8BwdLayout(int N, int I, int O, bool bf16)
@@ -124,6 +150,7 @@ struct Q8BwdLayout {
         strips = (int)((N + rows - 1) / rows);
         dw = q8_plan(O, I, 2 * nk, false);
         dx = q8_plan(N, I, planes * ok, false);
+        pair = q8_pair_tile(dx, dw, N, I, O, planes * ok, 2 * nk);
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
         colsum = take((size_t)strips * O * 4);
@@ -223,7 +250,7 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     q.col_exp = (int *)(at + l.cexp); q.row_exp = (int *)(at + l.rexp);
     q.aw = (_Float16 *)(at + l.aw); q.ax = (_Float16 *)(at + l.ax); q.bw = (_Float16 *)(at + l.bw); q.bx = (_Float16 *)(at + l.bx);
     q.nk = l.nk; q.ok = l.ok;
-    const long its = (d->I + 127) / 128, ts = (long)l.ok * l.strips, tx = its * l.nk, tw = want_dx ? its * l.ok : 0, tz = (long)l.nk * l.ok;
+    const long its = (d->I + 127) / 128, tz = (long)l.nk * l.ok, ts = (long)l.ok * l.strips, tx = its * l.nk, tw = want_dx ? its * l.ok : 0;
     if (ts + tx + tw > 0x7fffffffL || tz > 0x7fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 tiles of 64 x 64 values");
     q.tiles_s = (int)ts; q.tiles_x = (int)tx;
     auto prepare = [&](auto stat, auto halves) {
@@ -232,24 +259,33 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     };
     if (bf16) { if (want_dx) prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, 1>); else prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, 0>); }
     else { if (want_dx) prepare(q8_stat_kernel<float>, q8_prep_kernel<float, 2>); else prepare(q8_stat_kernel<float>, q8_prep_kernel<float, 0>); }
-    const hipError_t e = hipGetLastError();
+    hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
 
-    Q8GemmParams p;
-    memset(&p, 0, sizeof(p));
-    p.a = (const unsigned char *)q.aw; p.b = (const unsigned char *)q.bw;
-    p.lda = (size_t)l.nk * 256; p.ldb = (size_t)l.nk * 128;
-    p.M = ol; p.N = d->I; p.ksteps = 2 * l.nk; p.planes = 2;
-    p.out = dw; p.bf16 = 0;
-    p.d = {q.col_exp, alpha, beta};
-    OWT_TRY(run_product<Q8Half>(p, l.dw, at + l.partial, s));
-    if (!want_dx) return OWT_OK;
-    p.a = (const unsigned char *)q.ax; p.b = (const unsigned char *)q.bx;
-    p.lda = (size_t)l.ok * 128 * l.planes; p.ldb = (size_t)l.ok * 128;
-    p.M = d->N; p.N = d->I; p.ksteps = l.planes * l.ok; p.planes = l.planes;
-    p.out = dx_partial_or_null; p.bf16 = bf16;
-    p.d = {q.row_exp, 1.f, 0.f};
-    return run_product<Q8Half>(p, l.dx, at + l.partial, s);
+    Q8GemmParams w, x;          // dw, dx
+    memset(&w, 0, sizeof(w));
+    w.a = (const unsigned char *)q.aw; w.b = (const unsigned char *)q.bw;
+    w.lda = (size_t)l.nk * 256; w.ldb = (size_t)l.nk * 128;
+    w.M = ol; w.N = d->I; w.ksteps = 2 * l.nk; w.planes = 2;
+    w.out = dw; w.bf16 = 0;
+    w.d = {q.col_exp, alpha, beta};
+    x = w;
+    x.a = (const unsigned char *)q.ax; x.b = (const unsigned char *)q.bx;
+    x.lda = (size_t)l.ok * 128 * l.planes; x.ldb = (size_t)l.ok * 128;
+    x.M = d->N; x.ksteps = l.planes * l.ok; x.planes = l.planes;
+    x.out = dx_partial_or_null; x.bf16 = bf16;
+    x.d = {q.row_exp, 1.f, 0.f};
+    if (want_dx && l.pair) {
+        const Q8Plan pl{l.pair, 1, 0.f};
+        if (!lay_tiles(w, pl) || !lay_tiles(x, pl)) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+        const dim3 grid((unsigned)(owt_split_major_grid(x.tiles, 1) + owt_split_major_grid(w.tiles, 1)));
+        if (l.pair == 1) hipLaunchKernelGGL((q8gemm_pair_kernel<2, 2, 2, 2, 3, 1>), grid, dim3(256), 0, s, x, w);
+        else hipLaunchKernelGGL((q8gemm_pair_kernel<2, 2, 1, 1, 4, 2>), grid, dim3(256), 0, s, x, w);
+        e = hipGetLastError();
+        return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+    }
+    OWT_TRY(run_product<Q8Half>(w, l.dw, at + l.partial, s));
+    return want_dx ? run_product<Q8Half>(x, l.dx, at + l.partial, s) : OWT_OK;
 }
 
 }  // extern "C"

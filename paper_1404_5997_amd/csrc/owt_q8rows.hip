@@ -72,7 +72,7 @@ template <class T, bool RES> static void launch_bwd(const Q8NormBwdParams &p, co
     } else {
         if (f.p == 2) go(rmsnorm_bwd_kernel<T, RES, 1024, 2>);
         else if (f.p == 4) go(rmsnorm_bwd_kernel<T, RES, 1024, 4>);
-        else go(rmsnorm_bwd_kernel<T, RES, 1024, 8>);
+        else if constexpr (Piece<T>::V == 4) go(rmsnorm_bwd_kernel<T, RES, 1024, 8>);      // (16384 fp32 values and more)
     }
 }
 

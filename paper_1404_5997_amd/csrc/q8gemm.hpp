@@ -196,8 +196,8 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     const int ks_end = ks_beg + nst - 1;
     auto aim = [&](int ks, int buf) __attribute__((always_inline)) {
         ks = __builtin_amdgcn_readfirstlane(min(ks, ks_end));
-        ap = ag + (size_t)ks * 128;
-        bp = bg + (size_t)(p.planes == 2 ? ks >> 1 : ks) * 128;
+        ap = q8_uniform(ag + (size_t)ks * 128);
+        bp = q8_uniform(bg + (size_t)(p.planes == 2 ? ks >> 1 : ks) * 128);
         to = lds0 + buf * STAGE;
     };
     auto load = [&](int i) __attribute__((always_inline)) {
@@ -369,6 +369,21 @@ __global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_
     int tile, split;
     if (!owt_split_major_wg(p.tiles, p.splits, tile, split)) return;
     q8gemm_tile<Op, WM, WN, MB, NB, NS>(p, tile, split, lds);
+}
+
+// Both backward products in one launch, neither split: dx's tiles, whose sums are the longer ones in small shards, then dw's.
+template <int WM, int WN, int MB, int NB, int NS, int OCC>
+__global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_pair_kernel(const Q8GemmParams dx, const Q8GemmParams dw)
+{
+    __shared__ __attribute__((aligned(16))) unsigned char lds[NS * 32 * (MB * WM + NB * WN) * 128];
+    const int first = owt_split_major_grid(dx.tiles, 1), b = (int)blockIdx.x;
+    // (the numbering of owt_split_major_wg, within a product's work-groups: their number is a multiple of 8)
+    auto run = [&](const Q8GemmParams &p, int l) __attribute__((always_inline)) {
+        const int xcd = l & 7, jx = l >> 3, each = p.tiles >> 3, more = p.tiles & 7;
+        if (jx < each + (xcd < more ? 1 : 0)) q8gemm_tile<Q8Half, WM, WN, MB, NB, NS>(p, xcd * each + min(xcd, more) + jx, 0, lds);
+    };
+    if (b < first) run(dx, b);
+    else run(dw, b - first);
 }
 
 // Adds up the parts of a split sum, in order: four columns a thread.

@@ -8,8 +8,11 @@
 //
 // First launch: the whole numbers are turned, and dz is read once for the bias gradient's sums and the largest magnitudes of columns (times
 // xs) and rows (times ws), in parts of 64 columns x a strip of rows.  Second launch: the left operands, 64 x 64 values a work-group, the
-// one of dw turned through LDS.  Both are bound by memory: 8192 x 4096 -> 4096 in bf16 moves 490 MB.
+// one of dw turned through LDS.  Both are bound by memory: 8192 x 4096 -> 4096 in bf16 moves 490 MB in 115 us.  (One
+// launch for few rows and columns, each work-group finding the magnitudes of its own: 128 x 9216 -> 512 16 us where these two take 12.)
 #pragma once
+#include <type_traits>
+
 #include "owt_common.hpp"
 #include "q8piece.hpp"
 
@@ -35,15 +38,25 @@ struct Q8PrepParams {
     int tiles_s, tiles_x;               // work-groups of the first launch: statistics, then xq's tiles, then wq's
 };
 
-// dz of piece j of row n (zeros past the end of either)
-template <class T> __device__ __forceinline__ void q8_dz(const Q8PrepParams &p, int n, int j, float (&v)[Piece<T>::V])
+// dz of piece j of row n (zeros past the end of either).  HOW: 0 for any rows; 1 where rows are whole pieces and there are some, 2 where they
+// have a mask besides: then no load is behind a branch, and as many are on their way as a loop is unrolled to (behind branches they
+// wait for each other).
+template <class T, int HOW> __device__ __forceinline__ void q8_dz(const Q8PrepParams &p, int n, int j, float (&v)[Piece<T>::V])
 {
     constexpr int V = Piece<T>::V;
-    if (n >= p.N) {
+    const bool in = n < p.N && j * V < p.O;
+    if (HOW) {
+        const size_t at = (size_t)min(n, p.N - 1) * p.O + min(j, p.O / V - 1) * V;
+        Piece<T>::load((const T *)p.dy + at, v);
+        float y[V];
+        if (HOW == 2) Piece<T>::load((const T *)p.y + at, y);
 #pragma unroll
-        for (int i = 0; i < V; i++) v[i] = 0.f;
+        for (int i = 0; i < V; i++) v[i] = in && (HOW == 1 || y[i] > 0.f) ? v[i] : 0.f;
         return;
     }
+#pragma unroll
+    for (int i = 0; i < V; i++) v[i] = 0.f;
+    if (!in) return;
     load_piece<T>((const T *)p.dy + (size_t)n * p.O, j, p.O, v);
     if (p.y) {
         float y[V];
@@ -52,10 +65,16 @@ template <class T> __device__ __forceinline__ void q8_dz(const Q8PrepParams &p, 
         for (int i = 0; i < V; i++) v[i] = y[i] > 0.f ? v[i] : 0.f;
     }
 }
+template <class T, class F> __device__ __forceinline__ void q8_rows_are(const Q8PrepParams &p, F f)
+{
+    if (p.N <= 0 || p.O % Piece<T>::V) f(std::integral_constant<int, 0>{});
+    else if (p.y) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 1>{});
+}
 // what a value adds to a largest finite magnitude
 __device__ __forceinline__ float q8_finite_abs(float v) { return fabsf(v) < __uint_as_float(0x7f800000u) ? fabsf(v) : 0.f; }
 // the power of two that takes it to [2^14, 2^15)
-__device__ __forceinline__ int q8_exponent(float largest) { return largest > 0.f ? 14 - ilogbf(largest) : 0; }
+__device__ __forceinline__ int q8_exponent(float largest) { return largest > 0.f ? 15 - __builtin_amdgcn_frexp_expf(largest) : 0; }
 // v 2^e as two f16 values, the first in the low half
 __device__ __forceinline__ uint32_t q8_halves(float v, int e)
 {
@@ -65,7 +84,7 @@ __device__ __forceinline__ uint32_t q8_halves(float v, int e)
 }
 
 // The first launch's statistics: 64 columns of a strip of rows.  A wavefront reads 64 / LPR rows at a time, LPR lanes a row.
-template <class T> __device__ __forceinline__ void q8_stat(const Q8PrepParams &p, int cb, int strip, float *lds)
+template <class T, int HOW> __device__ __forceinline__ void q8_stat(const Q8PrepParams &p, int cb, int strip, float *lds)
 {
     constexpr int V = Piece<T>::V, LPR = 64 / V, RPW = 64 / LPR, AT = 4;      // AT pieces of a thread on their way at a time
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lc = lane % LPR, lr = lane / LPR, j = cb * LPR + lc;
@@ -81,8 +100,8 @@ template <class T> __device__ __forceinline__ void q8_stat(const Q8PrepParams &p
 #pragma unroll
         for (int a = 0; a < AT; a++) {
             const int n = n0 + a * RPW + lr;
-            xs[a] = n < n_end ? p.xs[n] : 0.f;
-            q8_dz<T>(p, n < n_end ? n : p.N, j, dz[a]);
+            xs[a] = p.xs[min(n, n_end - 1)];
+            q8_dz<T, HOW>(p, n < n_end ? n : p.N, j, dz[a]);
         }
 #pragma unroll
         for (int a = 0; a < AT; a++) {
@@ -163,7 +182,7 @@ template <class T> __global__ void __launch_bounds__(256) q8_stat_kernel(const Q
     __shared__ __attribute__((aligned(16))) unsigned lds[64 * 33];
     int b = blockIdx.x;
     const int its = (p.I + 127) / 128;
-    if (b < p.tiles_s) q8_stat<T>(p, b % p.ok, b / p.ok, (float *)lds);
+    if (b < p.tiles_s) q8_rows_are<T>(p, [&](auto how) __attribute__((always_inline)) { q8_stat<T, decltype(how)::value>(p, b % p.ok, b / p.ok, (float *)lds); });
     else if ((b -= p.tiles_s) < p.tiles_x) q8_turn(p.xq, p.xpitch, p.N, p.I, b / its, b % its, p.bw, p.nk, lds);
     else {
         b -= p.tiles_x;
@@ -171,18 +190,17 @@ template <class T> __global__ void __launch_bounds__(256) q8_stat_kernel(const Q
     }
 }
 
-template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel(const Q8PrepParams p)      // DX: planes of dx's operand, 0 = none
+// A 64 x 64 tile of dz.  DX: planes of dx's operand, 0 = none.
+template <class T, int DX, int HOW> __device__ __forceinline__ void q8_split(const Q8PrepParams &p, uint32_t *tile, int *ce, int *re)
 {
-    constexpr int V = Piece<T>::V, LPR = 64 / V, RPP = 256 / LPR, PASSES = 64 / RPP;    // lanes a row, rows a pass
-    __shared__ uint32_t tile[64 * 65];              // [n][o], both halves of a value in a word
-    __shared__ int ce[64], re[64];
+    constexpr int V = Piece<T>::V, LPR = 64 / V, RPP = 256 / LPR, PASSES = 64 / RPP;       // lanes a row, rows a pass
     const int tid = threadIdx.x, nt = blockIdx.x / p.ok, ot = blockIdx.x % p.ok, n0 = nt * 64, o0 = ot * 64;
     const int lc = tid % LPR, lr = tid / LPR;
     float dz[PASSES][V], ws[V], xs[PASSES];
 #pragma unroll
     for (int s = 0; s < PASSES; s++) {
         const int n = n0 + s * RPP + lr;
-        q8_dz<T>(p, n, ot * LPR + lc, dz[s]);
+        q8_dz<T, HOW>(p, n, ot * LPR + lc, dz[s]);
         xs[s] = n < p.N ? p.xs[n] : 0.f;
     }
 #pragma unroll
@@ -202,12 +220,12 @@ template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel
             p.col_exp[o] = ce[tid];
             if (p.db) p.db[o] = p.alpha * s + (p.beta != 0.f ? p.beta * p.db[o] : 0.f);
         }
-    } else if (tid < 128 && DX) {                   // and of the rows
-        const int n = n0 + tid - 64, cbs = p.ok;
+    } else if (DX && tid < 128) {           // and of the rows
+        const int n = n0 + tid - 64;
         float mx = 0.f;
         if (n < p.N)
 #pragma unroll 8
-            for (int k = 0; k < cbs; k++) mx = fmaxf(mx, p.rowmax[(size_t)k * p.N + n]);
+            for (int k = 0; k < p.ok; k++) mx = fmaxf(mx, p.rowmax[(size_t)k * p.N + n]);
         re[tid - 64] = q8_exponent(mx);
         if (ot == 0 && n < p.N) p.row_exp[n] = re[tid - 64];
     }
@@ -239,8 +257,8 @@ template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel
     }
     __syncthreads();
 #pragma unroll
-    for (int s = 0; s < 2; s++) {                   // eight tokens of an output a thread, eight threads a row of 64
-        const int oc = s * 32 + (tid >> 3), ko = tid & 7;
+    for (int at = 0; at < 512; at += 256) {         // eight tokens of an output a thread, eight threads a row of 64
+        const int oc = (at + tid) >> 3, ko = tid & 7;
         if (o0 + oc >= p.O) continue;
         uint32_t both[8];
 #pragma unroll
@@ -251,10 +269,17 @@ template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel
             h[j] = __builtin_amdgcn_perm(both[2 * j + 1], both[2 * j], 0x05040100u);
             m[j] = __builtin_amdgcn_perm(both[2 * j + 1], both[2 * j], 0x07060302u);
         }
-        _Float16 *at = p.aw + ((size_t)(o0 + oc) * p.nk + nt) * 128 + ko * 8;
-        *(uint4 *)at = make_uint4(h[0], h[1], h[2], h[3]);
-        *(uint4 *)(at + 64) = make_uint4(m[0], m[1], m[2], m[3]);
+        _Float16 *to = p.aw + ((size_t)(o0 + oc) * p.nk + nt) * 128 + ko * 8;
+        *(uint4 *)to = make_uint4(h[0], h[1], h[2], h[3]);
+        *(uint4 *)(to + 64) = make_uint4(m[0], m[1], m[2], m[3]);
     }
+}
+
+template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel(const Q8PrepParams p)
+{
+    __shared__ uint32_t tile[64 * 65];              // [n][o], both halves of a value in a word
+    __shared__ int ce[64], re[64];
+    q8_rows_are<T>(p, [&](auto how) __attribute__((always_inline)) { q8_split<T, DX, decltype(how)::value>(p, tile, ce, re); });
 }
 
 }  // namespace owt

@@ -302,7 +302,7 @@ class Shard:
 
 
 SHARDS = [(1, 1, 1), (1, 4096, 130), (2, 125, 33), (5, 640, 17), (16, 129, 512), (17, 300, 64), (63, 128, 65), (64, 127, 125), (65, 1000, 31),
-          (128, 9216, 125), (300, 257, 190), (520, 90, 300)]
+          (128, 9216, 125), (300, 257, 190), (520, 90, 300), (40, 70, 3000), (1500, 40, 70)]
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
