@@ -48,9 +48,9 @@ static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
         }
     }
     if (want_split > 0) best.splits = want_split < ksteps ? want_split : ksteps;
-    else if (forward && want < 0) {     // 16 x 16 results a work-group: 1.5 us and 0.08 a step (16 rows of 4096 -> 4096 take 7.2 us, tiles 9.7)
+    else if (forward && want < 0) {     // 16 x 16 results a work-group (us, this and the best of the tiles: 16 rows of 4096 -> 4096 5.2 and 9, 64 rows 11 and 10)
         const long tiles = ((M + 15) / 16) * ((N + 15) / 16);
-        if (3.f + (float)((tiles + 255) / 256) * (1.5f + 0.08f * (float)ksteps) < least) best = {kQ8Few, 1, 0.f};
+        if (3.f + (float)((tiles + 255) / 256) * (1.1f + 0.035f * (float)ksteps) < least) best = {kQ8Few, 1, 0.f};
     }
     return best;
 }

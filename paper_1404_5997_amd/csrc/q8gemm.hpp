@@ -149,6 +149,13 @@ __device__ __forceinline__ const unsigned char *q8_uniform(const unsigned char *
     return (const unsigned char *)(((unsigned long long)hi << 32) | lo);
 }
 
+// 16 bytes a lane from base + off straight into LDS: lane l's land at byte address `dst` (wave-uniform, in m0) + 16 l; the s_nop is the wait
+// state that the hardware wants between a scalar write of m0 and a load into LDS
+__device__ __forceinline__ void q8_load_lds(unsigned off, const unsigned char *base, unsigned dst)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
+}
+
 // One tile of C over the steps of `split`: WM x WN wavefronts of MB x NB blocks of 32 x 32; lds: NS stages.
 template <class Op, int WM, int WN, int MB, int NB, int NS>
 __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int split, unsigned char *lds)
@@ -184,11 +191,6 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     }
     const unsigned char *ag = q8_uniform(p.a + (size_t)m0 * p.lda), *bg = q8_uniform(p.b + (size_t)n0 * p.ldb);
 
-    // lane l's 16 bytes land at LDS byte address `dst` (wave-uniform, in m0) + 16 l; the s_nop is the wait state that the hardware wants
-    // between a scalar write of m0 and a load into LDS
-    auto dma16 = [&](unsigned off, const unsigned char *base, unsigned dst) __attribute__((always_inline)) {
-        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
-    };
     const unsigned lds0 = (unsigned)(size_t)(__attribute__((address_space(3))) unsigned char *)lds + wave * 1024;
     // the loads of step `ks` (past the last one: that again) into buffer `buf`: where from, and the i-th of them
     const unsigned char *ap, *bp;
@@ -201,13 +203,21 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
         to = lds0 + buf * STAGE;
     };
     auto load = [&](int i) __attribute__((always_inline)) {
-        if (i < AI) dma16(asrc[i < AI ? i : 0], ap, to + NW * i * 1024);
-        else dma16(bsrc[i < AI ? 0 : i - AI], bp, to + BM * 128 + NW * (i - AI) * 1024);
+        if (i < AI) q8_load_lds(asrc[i < AI ? i : 0], ap, to + NW * i * 1024);
+        else q8_load_lds(bsrc[i < AI ? 0 : i - AI], bp, to + BM * 128 + NW * (i - AI) * 1024);
     };
 
     unsigned fr[4];                                 // this lane's piece of a fragment's row, for each slice of 32 bytes
 #pragma unroll
     for (int kc = 0; kc < 4; kc++) fr[kc] = li * 128 + 16 * ((2 * kc + lh) ^ ((li >> 1) & 7));
+
+    // what the results need besides the sums is on its way from the start
+    constexpr int QW = 8 * NB, RT = (BM + 64 * NW - 1) / (64 * NW);     // 16-byte pieces of a wavefront's row of results; rows' scales of a thread
+    const int q = lane % QW, c = n0 + wn0 + 4 * q;
+    const Q8Cols k = q8_cols(p, c, typename Op::Acc());
+    int scale[RT];
+#pragma unroll
+    for (int i = 0; i < RT; i++) scale[i] = q8_row(p, m0 + tid + i * 64 * NW, typename Op::Acc());
 
     typename Op::Acc acc[MB][NB];
 #pragma unroll
@@ -283,14 +293,14 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     // from memory would wait for the stores before it.  A wavefront has its SIMD to itself here and an instruction
     // takes it 8 clocks, so they are few: no branch, no 64-bit address (the first form took 30000 clocks of the end of a 256 x 256 tile).
     typedef decltype(typename Op::Acc()[0] + 0) S;
-    constexpr int QW = 8 * NB, SW = QW < 16 ? QW - 1 : 15;              // pieces of a row, and the bits of its swizzle
+    constexpr int SW = QW < 16 ? QW - 1 : 15;       // the bits of a row's swizzle
     static_assert(NS * STAGE >= NW * 32 * QW * 16 + BM * 4, "32 rows of each wavefront and the rows' scales fit the stages");
     unsigned char *mine = lds + wave * (32 * QW * 16);
     int *rows = (int *)(lds + NW * (32 * QW * 16));
-    const int q = lane % QW, c = n0 + wn0 + 4 * q;
-    const Q8Cols k = q8_cols(p, c, typename Op::Acc());
     __syncthreads();                                // everybody has read the last stage
-    for (int i = tid; i < BM; i += 64 * NW) rows[i] = q8_row(p, m0 + i, typename Op::Acc());
+#pragma unroll
+    for (int i = 0; i < RT; i++)
+        if (tid + i * 64 * NW < BM) rows[tid + i * 64 * NW] = scale[i];
     __syncthreads();
     const unsigned width = (unsigned)p.N * (p.splits == 1 && p.bf16 ? 2 : 4);       // (rows of up to 2^24 bytes: 128 of them are addressed with 32 bits)
     unsigned char *base = (unsigned char *)q8_uniform((unsigned char *)(p.splits > 1 ? (char *)p.partial + (size_t)split * p.M * width : (char *)p.out) + (size_t)(m0 + wm0) * width);
