@@ -43,7 +43,7 @@ static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
             const long each = (tiles * sp + 255) / 256;         // work-groups of a CU
             const float step = tiles * sp >= (t == 0 ? 256 : 128) ? q.busy : q.step;
             float us = 3.f + (float)each * (q.start + (float)((ksteps + sp - 1) / sp) * step);
-            if (sp > 1) us += (N % 4 ? 5.6f : 3.6f) + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
+            if (sp > 1) us += 3.6f + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
             if (us < least) best = {t, sp, us};
         }
     }
@@ -67,8 +67,8 @@ static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long
         const Q8Tile &q = kQ8Tiles[t];
         const float tx = (float)(((N + q.bm - 1) / q.bm) * ((I + q.bn - 1) / q.bn)), tw = (float)(((O + q.bm - 1) / q.bm) * ((I + q.bn - 1) / q.bn));
         const float ux = q.start + (float)dx_steps * q.busy, uw = q.start + (float)dw_steps * q.busy;
-        float us = (tx * ux + tw * uw) / 256.f + 0.5f * (ux > uw ? ux : uw);
-        us = 3.f + (us > ux ? us : ux);
+        const float longest = ux > uw ? ux : uw, sum = (tx * ux + tw * uw) / 256.f + 0.2f * longest;
+        const float us = 3.f + (sum > longest ? sum : longest);
         if (us < least) { least = us; best = t; }
     }
     return best;
@@ -279,8 +279,10 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
         const Q8Plan pl{l.pair, 1, 0.f};
         if (!lay_tiles(w, pl) || !lay_tiles(x, pl)) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
         const dim3 grid((unsigned)(owt_split_major_grid(x.tiles, 1) + owt_split_major_grid(w.tiles, 1)));
-        if (l.pair == 1) hipLaunchKernelGGL((q8gemm_pair_kernel<2, 2, 2, 2, 3, 1>), grid, dim3(256), 0, s, x, w);
-        else hipLaunchKernelGGL((q8gemm_pair_kernel<2, 2, 1, 1, 4, 2>), grid, dim3(256), 0, s, x, w);
+        const bool dx_first = x.ksteps >= w.ksteps;
+        const Q8GemmParams &p0 = dx_first ? x : w, &p1 = dx_first ? w : x;
+        if (l.pair == 1) hipLaunchKernelGGL((q8gemm_pair_kernel<2, 2, 2, 2, 3, 1>), grid, dim3(256), 0, s, p0, p1);
+        else hipLaunchKernelGGL((q8gemm_pair_kernel<2, 2, 1, 1, 4, 2>), grid, dim3(256), 0, s, p0, p1);
         e = hipGetLastError();
         return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
     }

@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "owt_common.hpp"
+#include "q8piece.hpp"
 
 namespace owt {
 
@@ -61,17 +62,25 @@ struct Q8GemmParams {
     Q8BwdOut d;
 };
 
-// Four results C[m][c .. c + 3] of a row of N.  VEC: N is a multiple of four (then c is, too, and rows are aligned to four values); without it
-// the last ones may be past the row.
+// Four results C[m][c .. c + 3] of a row of N.  VEC: N is a multiple of four (then c is, too, and rows are aligned to four values).  Without
+// it rows begin anywhere, which memory takes as well, and the last of them may be past the row.
+struct __attribute__((packed, aligned(2))) Q8FourHalves { uint32_t lo, hi; };
 template <bool VEC, class T> __device__ __forceinline__ void q8_store4(T *row, int c, int N, const float (&v)[4])
 {
     if (VEC) {
         if (c >= N) return;
         if (sizeof(T) == 4) *(float4 *)((float *)row + c) = make_float4(v[0], v[1], v[2], v[3]);
         else *(uint2 *)((uint16_t *)row + c) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+    } else if (c + 4 <= N) {
+        if (sizeof(T) == 4) Piece<float>::store((float *)row + c, v);
+        else {
+            Q8FourHalves *to = (Q8FourHalves *)((uint16_t *)row + c);
+            to->lo = f32x2_to_bf16x2(v[0], v[1]);
+            to->hi = f32x2_to_bf16x2(v[2], v[3]);
+        }
     } else {
 #pragma unroll
-        for (int t = 0; t < 4; t++)
+        for (int t = 0; t < 3; t++)
             if (c + t < N) store1(row, (size_t)(c + t), v[t]);
     }
 }
@@ -80,10 +89,7 @@ template <bool VEC> __device__ __forceinline__ void q8_load4(const float *row, i
     if (VEC) {
         const float4 u = c < N ? *(const float4 *)(row + c) : make_float4(0.f, 0.f, 0.f, 0.f);
         v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-    } else {
-#pragma unroll
-        for (int t = 0; t < 4; t++) v[t] = c + t < N ? row[c + t] : 0.f;
-    }
+    } else load_piece<float>(row, c / 4, N, v);
 }
 // What four columns have in common for all rows, and a row for all columns: its scale, or its exponent.
 struct Q8Cols { float ws[4], bias[4]; };
@@ -303,7 +309,7 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
         if (tid + i * 64 * NW < BM) rows[tid + i * 64 * NW] = scale[i];
     __syncthreads();
     const unsigned width = (unsigned)p.N * (p.splits == 1 && p.bf16 ? 2 : 4);       // (rows of up to 2^24 bytes: 128 of them are addressed with 32 bits)
-    unsigned char *base = (unsigned char *)q8_uniform((unsigned char *)(p.splits > 1 ? (char *)p.partial + (size_t)split * p.M * width : (char *)p.out) + (size_t)(m0 + wm0) * width);
+    char *base = (p.splits > 1 ? (char *)p.partial + (size_t)split * p.M * width : (char *)p.out) + (size_t)(m0 + wm0) * width;
     const int m_end = __builtin_amdgcn_readfirstlane(max(0, min(32 * MB, p.M - m0 - wm0)));     // rows of this wavefront that exist
     const unsigned char *src = mine + lane / QW * (QW * 16);
     const int *factor = rows + wm0 + lane / QW;
@@ -325,7 +331,7 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
             constexpr int HOW = decltype(how)::value;
             constexpr unsigned SIZE = HOW == Q8_BF16 ? 2 : 4;
             // whole fours: through a descriptor that ends with the last row, where what lies outside is not written
-            const __amdgpu_buffer_rsrc_t rs = owt_make_rsrc(base, (unsigned)m_end * width);
+            const __amdgpu_buffer_rsrc_t rs = owt_make_rsrc(q8_uniform((const unsigned char *)base), (unsigned)m_end * width);
             unsigned at = c < p.N ? (unsigned)(32 * i + lane / QW) * width + (unsigned)c * SIZE : 0x80000000u;
             const unsigned step = c < p.N ? (64 / QW) * width : 0;
 #pragma nounroll
@@ -381,19 +387,19 @@ __global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_
     q8gemm_tile<Op, WM, WN, MB, NB, NS>(p, tile, split, lds);
 }
 
-// Both backward products in one launch, neither split: dx's tiles, whose sums are the longer ones in small shards, then dw's.
+// Both backward products in one launch, neither split: the one of longer sums first.
 template <int WM, int WN, int MB, int NB, int NS, int OCC>
-__global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_pair_kernel(const Q8GemmParams dx, const Q8GemmParams dw)
+__global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_pair_kernel(const Q8GemmParams p0, const Q8GemmParams p1)
 {
     __shared__ __attribute__((aligned(16))) unsigned char lds[NS * 32 * (MB * WM + NB * WN) * 128];
-    const int first = owt_split_major_grid(dx.tiles, 1), b = (int)blockIdx.x;
+    const int first = owt_split_major_grid(p0.tiles, 1), b = (int)blockIdx.x;
     // (the numbering of owt_split_major_wg, within a product's work-groups: their number is a multiple of 8)
     auto run = [&](const Q8GemmParams &p, int l) __attribute__((always_inline)) {
         const int xcd = l & 7, jx = l >> 3, each = p.tiles >> 3, more = p.tiles & 7;
         if (jx < each + (xcd < more ? 1 : 0)) q8gemm_tile<Q8Half, WM, WN, MB, NB, NS>(p, xcd * each + min(xcd, more) + jx, 0, lds);
     };
-    if (b < first) run(dx, b);
-    else run(dw, b - first);
+    if (b < first) run(p0, b);
+    else run(p1, b - first);
 }
 
 // Adds up the parts of a split sum, in order: four columns a thread.

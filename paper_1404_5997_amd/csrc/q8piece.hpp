@@ -57,6 +57,19 @@ template <class T> __device__ __forceinline__ void load_piece(const T *row, int 
         for (int i = 0; i < V; i++) v[i] = c + i < cols ? load1(row, c + i) : 0.f;
     }
 }
+// The same where a row's last values would wait for each other behind their branches (for more registers).
+template <class T> __device__ __forceinline__ void load_piece_at_once(const T *row, int j, int cols, float (&v)[Piece<T>::V])
+{
+    constexpr int V = Piece<T>::V;
+    const int c = j * V;
+    if (c + V <= cols) Piece<T>::load(row + c, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = load1(row, min(c + i, cols - 1));
+#pragma unroll
+        for (int i = 0; i < V; i++) v[i] = c + i < cols ? v[i] : 0.f;
+    }
+}
 template <class T> __device__ __forceinline__ void store_piece(T *row, int j, int cols, const float (&v)[Piece<T>::V])
 {
     constexpr int V = Piece<T>::V;

@@ -57,10 +57,10 @@ template <class T, int HOW> __device__ __forceinline__ void q8_dz(const Q8PrepPa
 #pragma unroll
     for (int i = 0; i < V; i++) v[i] = 0.f;
     if (!in) return;
-    load_piece<T>((const T *)p.dy + (size_t)n * p.O, j, p.O, v);
+    load_piece_at_once<T>((const T *)p.dy + (size_t)n * p.O, j, p.O, v);
     if (p.y) {
         float y[V];
-        load_piece<T>((const T *)p.y + (size_t)n * p.O, j, p.O, y);
+        load_piece_at_once<T>((const T *)p.y + (size_t)n * p.O, j, p.O, y);
 #pragma unroll
         for (int i = 0; i < V; i++) v[i] = y[i] > 0.f ? v[i] : 0.f;
     }
@@ -205,29 +205,35 @@ template <class T, int DX, int HOW> __device__ __forceinline__ void q8_split(con
     }
 #pragma unroll
     for (int i = 0; i < V; i++) ws[i] = o0 + lc * V + i < p.O ? p.ws[o0 + lc * V + i] : 0.f;
-    if (tid < 64) {                                 // exponents of the columns; the bias gradient
-        const int o = o0 + tid;
-        float mx = 0.f, s = 0.f;
+    {   // largest magnitudes of the tile's columns and rows, and the bias gradient: each by four threads, every fourth part
+        float *red = (float *)tile;                 // [3][4][64], before the tile
+        const int i = tid & 63, part = tid >> 6, o = o0 + i, n = n0 + i;
+        float cmax = 0.f, sum = 0.f, rmax = 0.f;
         if (o < p.O) {
 #pragma unroll 8
-            for (int k = 0; k < p.strips; k++) mx = fmaxf(mx, p.colmax[(size_t)k * p.O + o]);
+            for (int k = part; k < p.strips; k += 4) cmax = fmaxf(cmax, p.colmax[(size_t)k * p.O + o]);
             if (nt == 0)
 #pragma unroll 8
-                for (int k = 0; k < p.strips; k++) s += p.colsum[(size_t)k * p.O + o];
+                for (int k = part; k < p.strips; k += 4) sum += p.colsum[(size_t)k * p.O + o];
         }
-        ce[tid] = q8_exponent(mx);
-        if (nt == 0 && o < p.O) {
-            p.col_exp[o] = ce[tid];
-            if (p.db) p.db[o] = p.alpha * s + (p.beta != 0.f ? p.beta * p.db[o] : 0.f);
-        }
-    } else if (DX && tid < 128) {           // and of the rows
-        const int n = n0 + tid - 64;
-        float mx = 0.f;
-        if (n < p.N)
+        if (DX && n < p.N)
 #pragma unroll 8
-            for (int k = 0; k < p.ok; k++) mx = fmaxf(mx, p.rowmax[(size_t)k * p.N + n]);
-        re[tid - 64] = q8_exponent(mx);
-        if (ot == 0 && n < p.N) p.row_exp[n] = re[tid - 64];
+            for (int k = part; k < p.ok; k += 4) rmax = fmaxf(rmax, p.rowmax[(size_t)k * p.N + n]);
+        red[tid] = cmax; red[256 + tid] = sum; red[512 + tid] = rmax;
+        __syncthreads();
+        if (tid < 64) {
+            const int e = q8_exponent(fmaxf(fmaxf(red[i], red[64 + i]), fmaxf(red[128 + i], red[192 + i])));
+            ce[i] = e;
+            if (nt == 0 && o < p.O) {
+                p.col_exp[o] = e;
+                const float s = (red[256 + i] + red[320 + i]) + (red[384 + i] + red[448 + i]);
+                if (p.db) p.db[o] = p.alpha * s + (p.beta != 0.f ? p.beta * p.db[o] : 0.f);
+            }
+        } else if (DX && tid < 128) {
+            const int e = q8_exponent(fmaxf(fmaxf(red[512 + i], red[576 + i]), fmaxf(red[640 + i], red[704 + i])));
+            re[i] = e;
+            if (ot == 0 && n < p.N) p.row_exp[n] = e;
+        }
     }
     __syncthreads();
 #pragma unroll
