@@ -84,6 +84,7 @@ static bool lay_tiles(Q8GemmParams &p, const Q8Plan &pl)
     const long tiles = (long)p.tiles_n * ((p.M + q.bm - 1) / q.bm);
     p.tiles = (int)tiles;
     p.splits = pl.splits;
+    p.big = (size_t)p.M * p.N * (p.bf16 ? 2 : 4) > (32u << 20);
     p.ksteps_per_split = ((p.ksteps / p.planes + pl.splits - 1) / pl.splits) * p.planes;
     return tiles * pl.splits <= 0x3fffffffL;
 }

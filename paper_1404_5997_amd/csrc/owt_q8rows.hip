@@ -8,24 +8,33 @@
 namespace owt {
 
 // A row of n pieces: threads a row and pieces a thread.  Rows of up to 64 threads need no barrier, and short ones share a wavefront.
-template <class T, bool NORM, bool RES>
-static void launch_rows(const Q8RowParams &p, hipStream_t s)
+// more than an eighth of the 256 MB behind the L2 caches
+template <class T> static bool big(int rows, int cols) { return (size_t)rows * cols * sizeof(T) > (32u << 20); }
+
+template <class T, bool NORM, bool RES, bool BIG>
+static void launch_rows_as(const Q8RowParams &p, hipStream_t s)
 {
     const long n = (long)(p.pitch / Piece<T>::V);
     auto go = [&](auto kernel, int tpr) {
         const int threads = tpr > 256 ? tpr : 256, rpw = threads / tpr;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((p.rows + rpw - 1) / rpw)), dim3(threads), 0, s, p);
     };
-    if (n <= 16) go(q8_rows_kernel<T, NORM, RES, 16, 1, false>, 16);
-    else if (n <= 32) go(q8_rows_kernel<T, NORM, RES, 32, 1, false>, 32);
-    else if (n <= 64) go(q8_rows_kernel<T, NORM, RES, 64, 1, false>, 64);
-    else if (n <= 128) go(q8_rows_kernel<T, NORM, RES, 64, 2, false>, 64);
-    else if (n <= 256) go(q8_rows_kernel<T, NORM, RES, 64, 4, false>, 64);
-    else if (n <= 512) go(q8_rows_kernel<T, NORM, RES, 256, 2, false>, 256);
-    else if (n <= 1024) go(q8_rows_kernel<T, NORM, RES, 256, 4, false>, 256);
-    else if (n <= 2048) go(q8_rows_kernel<T, NORM, RES, 1024, 2, false>, 1024);
-    else if (n <= 4096) go(q8_rows_kernel<T, NORM, RES, 1024, 4, false>, 1024);
-    else go(q8_rows_kernel<T, NORM, RES, 1024, 1, true>, 1024);
+    if (n <= 16) go(q8_rows_kernel<T, NORM, RES, 16, 1, false, BIG>, 16);
+    else if (n <= 32) go(q8_rows_kernel<T, NORM, RES, 32, 1, false, BIG>, 32);
+    else if (n <= 64) go(q8_rows_kernel<T, NORM, RES, 64, 1, false, BIG>, 64);
+    else if (n <= 128) go(q8_rows_kernel<T, NORM, RES, 64, 2, false, BIG>, 64);
+    else if (n <= 256) go(q8_rows_kernel<T, NORM, RES, 64, 4, false, BIG>, 64);
+    else if (n <= 512) go(q8_rows_kernel<T, NORM, RES, 256, 2, false, BIG>, 256);
+    else if (n <= 1024) go(q8_rows_kernel<T, NORM, RES, 256, 4, false, BIG>, 256);
+    else if (n <= 2048) go(q8_rows_kernel<T, NORM, RES, 1024, 2, false, BIG>, 1024);
+    else if (n <= 4096) go(q8_rows_kernel<T, NORM, RES, 1024, 4, false, BIG>, 1024);
+    else go(q8_rows_kernel<T, NORM, RES, 1024, 1, true, BIG>, 1024);
+}
+
+template <class T, bool NORM, bool RES> static void launch_rows(const Q8RowParams &p, hipStream_t s)
+{
+    if (big<T>(p.rows, p.cols)) launch_rows_as<T, NORM, RES, true>(p, s);
+    else launch_rows_as<T, NORM, RES, false>(p, s);
 }
 
 template <class T> static void launch_unpack(const signed char *q, const float *scale, void *x, int rows, int cols, hipStream_t s)
@@ -58,22 +67,28 @@ static BwdShape bwd_shape(int cols, int v)
 }
 constexpr int kNormMaxCols = 32768;
 
-template <class T, bool RES> static void launch_bwd(const Q8NormBwdParams &p, const BwdShape &f, hipStream_t s)
+template <class T, bool RES, bool BIG> static void launch_bwd_as(const Q8NormBwdParams &p, const BwdShape &f, hipStream_t s)
 {
     auto go = [&](auto kernel) {
         const int threads = f.tpr > 256 ? f.tpr : 256, spw = threads / f.tpr;
         hipLaunchKernelGGL(kernel, dim3((unsigned)((p.strips + spw - 1) / spw)), dim3(threads), 0, s, p);
     };
-    if (f.tpr == 64) { if (f.p == 1) go(rmsnorm_bwd_kernel<T, RES, 64, 1>); else go(rmsnorm_bwd_kernel<T, RES, 64, 2>); }
+    if (f.tpr == 64) { if (f.p == 1) go(rmsnorm_bwd_kernel<T, RES, 64, 1, BIG>); else go(rmsnorm_bwd_kernel<T, RES, 64, 2, BIG>); }
     else if (f.tpr == 256) {
-        if (f.p == 1) go(rmsnorm_bwd_kernel<T, RES, 256, 1>);
-        else if (f.p == 2) go(rmsnorm_bwd_kernel<T, RES, 256, 2>);
-        else go(rmsnorm_bwd_kernel<T, RES, 256, 4>);
+        if (f.p == 1) go(rmsnorm_bwd_kernel<T, RES, 256, 1, BIG>);
+        else if (f.p == 2) go(rmsnorm_bwd_kernel<T, RES, 256, 2, BIG>);
+        else go(rmsnorm_bwd_kernel<T, RES, 256, 4, BIG>);
     } else {
-        if (f.p == 2) go(rmsnorm_bwd_kernel<T, RES, 1024, 2>);
-        else if (f.p == 4) go(rmsnorm_bwd_kernel<T, RES, 1024, 4>);
-        else if constexpr (Piece<T>::V == 4) go(rmsnorm_bwd_kernel<T, RES, 1024, 8>);      // (16384 fp32 values and more)
+        if (f.p == 2) go(rmsnorm_bwd_kernel<T, RES, 1024, 2, BIG>);
+        else if (f.p == 4) go(rmsnorm_bwd_kernel<T, RES, 1024, 4, BIG>);
+        else if constexpr (Piece<T>::V == 4) go(rmsnorm_bwd_kernel<T, RES, 1024, 8, BIG>);      // (16384 fp32 values and more)
     }
+}
+
+template <class T, bool RES> static void launch_bwd(const Q8NormBwdParams &p, const BwdShape &f, hipStream_t s)
+{
+    if (big<T>(p.rows, p.cols)) launch_bwd_as<T, RES, true>(p, f, s);
+    else launch_bwd_as<T, RES, false>(p, f, s);
 }
 
 static owt_status check_rows(int rows, int cols, owt_dtype dtype)
