@@ -21,9 +21,16 @@ static const Q8Tile kQ8Tiles[kNumQ8Tiles] = {{256, 256, 11.f, 1.05f, 1.5f}, {128
 template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, hipStream_t s)
 {
     const dim3 grid((unsigned)owt_split_major_grid(p.tiles, p.splits));
-    if (t == 0) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 4, 4, 2, 1>), grid, dim3(256), 0, s, p);
-    else if (t == 1) hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 2, 2, 3, 1>), grid, dim3(256), 0, s, p);
-    else hipLaunchKernelGGL((q8gemm_kernel<Op, 2, 2, 1, 1, 4, 2>), grid, dim3(256), 0, s, p);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p); };
+    if (t == 0) {
+        bool paired = false;
+        if constexpr (std::is_same<Op, Q8Half>::value) {
+            paired = p.planes == 2;
+            if (paired) go(q8gemm_kernel<Op, 2, 2, 4, 4, 5, true, 1>);
+        }
+        if (!paired) go(q8gemm_kernel<Op, 2, 2, 4, 4, 2, false, 1>);
+    } else if (t == 1) go(q8gemm_kernel<Op, 2, 2, 2, 2, 3, false, 1>);
+    else go(q8gemm_kernel<Op, 2, 2, 1, 1, 4, false, 2>);
     return hipGetLastError();
 }
 

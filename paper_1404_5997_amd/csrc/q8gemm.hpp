@@ -166,15 +166,21 @@ __device__ __forceinline__ void q8_load_lds(unsigned off, const unsigned char *b
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
 }
 
-// One tile of C over the steps of `split`: WM x WN wavefronts of MB x NB blocks of 32 x 32; lds: NS stages.
-template <class Op, int WM, int WN, int MB, int NB, int NS>
+// One tile of C over the steps of `split`: WM x WN wavefronts of MB x NB blocks of 32 x 32; lds: NS stages of both operands' tiles of a step.
+//
+// PAIRS: the steps of A go in pairs that meet the same step of B, and lds holds NS tiles of one operand, filled one by one in the order they
+// are used.  256 x 256 results take 32 KB of either operand a step, so that two stages are all that LDS holds; this way B is loaded once for a
+// pair, its fragments, read from LDS with the first plane, stay in registers for the second, and with five tiles a load has two products of
+// a step to arrive in instead of less than one (dw of 8192 x 4096 -> 4096 432 us, 466 by stages; one plane by five tiles 244 us, 231 by stages).
+template <class Op, int WM, int WN, int MB, int NB, int NS, bool PAIRS>
 __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int split, unsigned char *lds)
 {
     constexpr int NW = WM * WN, BM = 32 * MB * WM, BN = 32 * NB * WN;
     constexpr int AI = BM / 8 / NW, BI = BN / 8 / NW, L = AI + BI;     // loads of a wavefront and stage
     static_assert((BM / 8) % NW == 0 && (BN / 8) % NW == 0, "every wavefront issues the same number of loads");
-    static_assert(NS >= 2 && (NS - 1) * L <= 63, "the wait counter has six bits");
-    constexpr int STAGE = (BM + BN) * 128;
+    static_assert(NS >= 2 && (PAIRS ? 3 * AI : (NS - 1) * L) <= 63, "the wait counter has six bits");
+    static_assert(!PAIRS || (BM == BN && NS == 5), "tiles of one size, five of them");
+    constexpr int STAGE = PAIRS ? BM * 128 : (BM + BN) * 128;
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int li = lane & 31, lh = lane >> 5;
@@ -237,65 +243,111 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
 #pragma unroll
             for (int r = 0; r < 16; r++) acc[i][j][r] = 0;
 
-    // A slice: its products, and between them the reads of the next slice's fragments (slice kc of buffer `buf`) and, in a stage's last
-    // one, the loads of another stage.  The order is kept as written: the compiler would gather the reads in front of
-    // the products that wait for them.
-    q8_i32x4 af[2][MB], bf[2][NB];
-    auto read1 = [&](int f, int kc, int buf, int side) __attribute__((always_inline)) {
-        const unsigned char *at = lds + buf * STAGE + fr[kc];
-        if (f < MB) af[side][f < MB ? f : 0] = *(const q8_i32x4 *)(at + (wm0 + 32 * f) * 128);
-        else bf[side][f < MB ? 0 : f - MB] = *(const q8_i32x4 *)(at + (BM + wn0 + 32 * (f - MB)) * 128);
-    };
-    auto slice = [&](int side, bool reads, int kc, int buf, bool loads) __attribute__((always_inline)) {
-        constexpr int P = MB * NB, F = MB + NB;
+    // A slice of 32 bytes: its products, and between them the reads of the next slice's fragments and, in a step's last one, loads.  The order is
+    // kept as written: the compiler would gather the reads in front of the products that wait for them.
+    constexpr int P = MB * NB;
+    q8_i32x4 af[2][MB], bf[PAIRS ? 4 : 2][NB];
+    auto read = [&](q8_i32x4 &to, int tile_at, int row, int kc) __attribute__((always_inline)) { to = *(const q8_i32x4 *)(lds + tile_at + row * 128 + fr[kc]); };
+    // products of af[a] and bf[b]; reads f = 0 .. reads - 1 by `reader`, loads i = 0 .. loads - 1 by `loader`
+    auto slice = [&](int a, int b, int reads, auto reader, int loads, auto loader) __attribute__((always_inline)) {
 #pragma unroll
         for (int t = 0; t < P; t++) {
-            if (reads)
 #pragma unroll
-                for (int f = 0; f < F; f++)
-                    if (f * P / F == t) read1(f, kc, buf, side ^ 1);
-            acc[t / NB][t % NB] = Op::mul(bf[side][t % NB], af[side][t / NB], acc[t / NB][t % NB]);
-            if (loads)
+            for (int f = 0; f < MB + NB; f++)
+                if (f < reads && f * P / reads == t) reader(f);
+            acc[t / NB][t % NB] = Op::mul(bf[b][t % NB], af[a][t / NB], acc[t / NB][t % NB]);
 #pragma unroll
-                for (int i = 0; i < L; i++)
-                    if (i * P / L == t) load(i);
+            for (int i = 0; i < L; i++)
+                if (i < loads && i * P / loads == t) loader(i);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
-
-    // s_waitcnt vmcnt(k stages' loads) lgkmcnt(0), expcnt untouched; then the same of all wavefronts
-#define OWT_WAIT_STAGES(k) __builtin_amdgcn_s_waitcnt((((k) * L) & 15) | ((((k) * L) >> 4) << 14) | (7 << 4))
-    if (nst > 0) {
+    auto nothing = [](int) __attribute__((always_inline)) {};
+    // s_waitcnt vmcnt(n) lgkmcnt(0), expcnt untouched; then the same of all wavefronts
+#define OWT_ARRIVED(n) do { asm volatile("" ::: "memory"); __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4)); \
+                            __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); } while (0)
+    if constexpr (PAIRS) {
+        const int pairs = nst / 2;
+        auto place = [](int slot) __attribute__((always_inline)) { return slot * STAGE; };
+        auto turn = [](int slot, int by) __attribute__((always_inline)) { slot += by; return slot >= 5 ? slot - 5 : slot; };
+        auto a_from = [&](int ks) __attribute__((always_inline)) { return q8_uniform(ag + (size_t)__builtin_amdgcn_readfirstlane(min(ks, ks_beg + nst - 2 + (ks & 1))) * 128); };
+        auto b_from = [&](int t) __attribute__((always_inline)) { return q8_uniform(bg + (size_t)__builtin_amdgcn_readfirstlane(ks_beg / 2 + min(t, pairs - 1)) * 128); };
+        auto load_a = [&](const unsigned char *from, int slot, int i) __attribute__((always_inline)) { q8_load_lds(asrc[i], from, lds0 + place(slot) + NW * i * 1024); };
+        auto load_b = [&](const unsigned char *from, int slot, int i) __attribute__((always_inline)) { q8_load_lds(bsrc[i], from, lds0 + place(slot) + NW * i * 1024); };
+        if (nst > 0) {
+            // B of pair t lies in slot 3 t, the two planes of A in 3 t + 1 and 3 t + 2 (modulo five).  Behind the first plane the first two of them
+            // are the second plane of pair t + 1 and B of pair t + 2, behind the second the third is the first plane of pair t + 2.
+            int sb = 0;
+#pragma unroll
+            for (int id = 0; id < 5; id++)
+#pragma unroll
+                for (int i = 0; i < AI; i++) {
+                    if (id % 3 == 0) load_b(b_from(id / 3), id, i);
+                    else load_a(a_from(ks_beg + 2 * (id / 3) + id % 3 - 1), id, i);
+                }
+            OWT_ARRIVED(3 * AI);
+#pragma unroll
+            for (int f = 0; f < MB; f++) read(af[0][f], place(1), wm0 + 32 * f, 0);
+#pragma unroll
+            for (int f = 0; f < NB; f++) read(bf[0][f], place(0), wn0 + 32 * f, 0);
+            for (int t = 0; t < pairs; t++) {
+                const int sh = turn(sb, 1), sm = turn(sb, 2), nb = turn(sb, 3), nh = turn(sb, 4);
+#pragma unroll
+                for (int kc = 0; kc < 3; kc++)
+                    slice(kc & 1, kc, MB + NB, [&](int f) __attribute__((always_inline)) {
+                        if (f < MB) read(af[(kc & 1) ^ 1][f < MB ? f : 0], place(sh), wm0 + 32 * f, kc + 1);
+                        else read(bf[PAIRS ? kc + 1 : 0][f < MB ? 0 : f - MB], place(sb), wn0 + 32 * (f - MB), kc + 1);
+                    }, 0, nothing);
+                // The second plane is there, and everybody has the last fragments of the first and of B.  (The last pairs load the last one again, and
+                // the very last reads fragments that nothing uses: a second copy of this code would take longer to arrive than that does.)
+                OWT_ARRIVED(2 * AI);
+                const unsigned char *fm = a_from(ks_beg + 2 * t + 3), *fb = b_from(t + 2), *fh = a_from(ks_beg + 2 * t + 4);
+                slice(1, PAIRS ? 3 : 0, MB, [&](int f) __attribute__((always_inline)) { read(af[0][f < MB ? f : 0], place(sm), wm0 + 32 * f, 0); },
+                      L, [&](int i) __attribute__((always_inline)) {
+                          if (i < AI) load_a(fm, sb, i < AI ? i : 0);
+                          else load_b(fb, sh, i < AI ? 0 : i - AI);
+                      });
+#pragma unroll
+                for (int kc = 0; kc < 3; kc++)
+                    slice(kc & 1, kc, MB, [&](int f) __attribute__((always_inline)) { read(af[(kc & 1) ^ 1][f < MB ? f : 0], place(sm), wm0 + 32 * f, kc + 1); }, 0, nothing);
+                OWT_ARRIVED(2 * AI);
+                slice(1, PAIRS ? 3 : 0, MB + NB, [&](int f) __attribute__((always_inline)) {
+                    if (f < MB) read(af[0][f < MB ? f : 0], place(nh), wm0 + 32 * f, 0);
+                    else read(bf[0][f < MB ? 0 : f - MB], place(nb), wn0 + 32 * (f - MB), 0);
+                }, AI, [&](int i) __attribute__((always_inline)) { load_a(fh, sm, i < AI ? i : 0); });
+                sb = nb;
+            }
+        }
+    } else if (nst > 0) {
 #pragma unroll
         for (int s = 0; s < NS; s++) {
             aim(ks_beg + s, s);
 #pragma unroll
             for (int i = 0; i < L; i++) load(i);
         }
-        OWT_WAIT_STAGES(NS - 1);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+        OWT_ARRIVED((NS - 1) * L);
+        auto reads = [&](int side, int kc, int buf) __attribute__((always_inline)) {
+            return [&, side, kc, buf](int f) __attribute__((always_inline)) {
+                if (f < MB) read(af[side][f < MB ? f : 0], buf * STAGE, wm0 + 32 * f, kc);
+                else read(bf[side][f < MB ? 0 : f - MB], buf * STAGE, BM + wn0 + 32 * (f - MB), kc);
+            };
+        };
 #pragma unroll
-        for (int f = 0; f < MB + NB; f++) read1(f, 0, 0, 0);
+        for (int f = 0; f < MB + NB; f++) reads(0, 0, 0)(f);
         int cur = 0;                                // stage s lives in buffer s % NS
         for (int s = 0; s < nst; s++) {
             const int next = cur == NS - 1 ? 0 : cur + 1;
 #pragma unroll
-            for (int kc = 0; kc < 3; kc++) slice(kc & 1, true, kc + 1, cur, false);
-            // Stage s + 1 has landed and everybody has this stage's last fragments: its buffer is filled anew.  (The last stages load the last
-            // step again, and the very last reads fragments of it that nothing uses: a second copy of this code would take longer to arrive
-            // than that does.)
-            asm volatile("" ::: "memory");
-            OWT_WAIT_STAGES(NS - 2);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
+            for (int kc = 0; kc < 3; kc++) slice(kc & 1, kc & 1, MB + NB, reads((kc & 1) ^ 1, kc + 1, cur), 0, nothing);
+            // stage s + 1 has landed and everybody has this stage's last fragments: its buffer is filled anew (the last ones as above)
+            OWT_ARRIVED((NS - 2) * L);
             aim(ks_beg + s + NS, cur);
-            slice(1, true, 0, next, true);
+            slice(1, 1, MB + NB, reads(0, 0, next), L, load);
             cur = next;
         }
-        __builtin_amdgcn_s_waitcnt(0x0F70);         // vmcnt(0): the last loads into LDS have landed, too
     }
-#undef OWT_WAIT_STAGES
+    __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0): the last loads into LDS have landed, too
+#undef OWT_ARRIVED
 
     // Accumulator register r of lane (li, lh): column 8 (r / 4) + 4 lh + r % 4 of C, row li of its block (the operands change places in the
     // instruction): four neighbouring results a lane.  They go through LDS, 32 rows of a wavefront at a time, so that rows are written as
@@ -383,13 +435,13 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     }
 }
 
-template <class Op, int WM, int WN, int MB, int NB, int NS, int OCC>
+template <class Op, int WM, int WN, int MB, int NB, int NS, bool PAIRS, int OCC>
 __global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_kernel(const Q8GemmParams p)
 {
-    __shared__ __attribute__((aligned(16))) unsigned char lds[NS * 32 * (MB * WM + NB * WN) * 128];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[NS * 32 * (MB * WM + (PAIRS ? 0 : NB * WN)) * 128];
     int tile, split;
     if (!owt_split_major_wg(p.tiles, p.splits, tile, split)) return;
-    q8gemm_tile<Op, WM, WN, MB, NB, NS>(p, tile, split, lds);
+    q8gemm_tile<Op, WM, WN, MB, NB, NS, PAIRS>(p, tile, split, lds);
 }
 
 // Both backward products in one launch, neither split: the one of longer sums first.
@@ -401,7 +453,7 @@ __global__ void __launch_bounds__(64 * WM * WN, (OCC * WM * WN + 3) / 4) q8gemm_
     // (the numbering of owt_split_major_wg, within a product's work-groups: their number is a multiple of 8)
     auto run = [&](const Q8GemmParams &p, int l) __attribute__((always_inline)) {
         const int xcd = l & 7, jx = l >> 3, each = p.tiles >> 3, more = p.tiles & 7;
-        if (jx < each + (xcd < more ? 1 : 0)) q8gemm_tile<Q8Half, WM, WN, MB, NB, NS>(p, xcd * each + min(xcd, more) + jx, 0, lds);
+        if (jx < each + (xcd < more ? 1 : 0)) q8gemm_tile<Q8Half, WM, WN, MB, NB, NS, false>(p, xcd * each + min(xcd, more) + jx, 0, lds);
     };
     if (b < first) run(p0, b);
     else run(p1, b - first);
