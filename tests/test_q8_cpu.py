@@ -86,3 +86,30 @@ def test_int8_tensors_have_to_be_dense(m):
     torch = pytest.importorskip("torch")
     with pytest.raises(ValueError):
         m.owt_q8_pack(4, 64, m.OWT_F32, torch.zeros((4, 128))[:, :64], 256, 512, 0)
+
+
+def test_every_barrier_of_the_products_waits_for_the_reads_before_it(tmp_path):
+    """As the compiler leaves them: behind a barrier in a product's walk loads overwrite a tile that fragments were read from, so each
+    wavefront has to have its reads behind it (and its loads, to the count that may stay) when it comes there."""
+    import importlib.util
+    import os
+    import re
+    import subprocess
+    package = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_1404_5997_amd")
+    spec = importlib.util.spec_from_file_location("_owt_build", os.path.join(package, "build.py"))
+    build = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(build)
+    out = str(tmp_path / "k.s")
+    subprocess.run([build.HIPCC] + build.FLAGS + ["--cuda-device-only", "-S", "-o", out, os.path.join(build.CSRC, "owt_q8fc.hip")], check=True, capture_output=True)
+    with open(out) as f:
+        kernels = re.findall(r"^(_ZN3owt1\dq8gemm_(?:pair_)?kernel\w+):(.*?)^\.Lfunc_end", f.read(), re.M | re.S)
+    assert len(kernels) == 9
+    for name, body in kernels:
+        code = [l.strip() for l in body.splitlines() if l.startswith("\t") and not l.strip().startswith((";", "."))]
+        for walk in re.split(r"\n(?=ds_write)", "\n".join(code)):           # (results go through LDS behind the walk)
+            walk = walk.splitlines()
+            loads = [i for i, l in enumerate(walk) if l.startswith("global_load_lds")]
+            barriers = [i for i, l in enumerate(walk) if l.startswith("s_barrier") and loads and loads[0] < i < loads[-1]]
+            for b in barriers:
+                assert re.fullmatch(r"s_waitcnt vmcnt\(\d+\) lgkmcnt\(0\)", walk[b - 1]), (name, walk[b - 3:b + 1])
+            assert not loads or barriers, name
