@@ -312,8 +312,9 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
  * dy, y [N][O_local], dx_partial [N][I] in the descriptor's dtype; dw [O_local][I] (dense, no pitch) and dbias fp32.
  * dz times its scale is multiplied as the sum of two f16 values under a power of two for each row of a result, which hold 22 bits of all
  * that is within 2^-16 of the row's largest such value, and 2^-39 of the largest below that; one f16 value (11 bits) for dx in bf16.
- * ws: owt_fc_shard_q8_workspace_bytes of OWT_PASS_BWD_DATA (one figure for the whole pass), about 2 to 4 bytes for every value of xq and
- * wq and 2 to 8 for every value of dz. */
+ * Where there is little to multiply it is the sum of three bf16 values, which hold all 24 bits; two (16 bits) for dx in bf16.
+ * ws: owt_fc_shard_q8_workspace_bytes of OWT_PASS_BWD_DATA (one figure for the whole pass, whichever kernels serve it), about 2 to 4 bytes
+ * for every value of xq and wq and 2 to 8 for every value of dz. */
 owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
                                const void *y_or_null, const void *dy, float alpha, float beta, void *dx_partial_or_null, float *dw,
                                float *dbias_or_null, void *ws, size_t ws_bytes, void *hip_stream);
@@ -338,7 +339,7 @@ const char *owt_last_error(void);
  * 80..86 stride-1 filter gradient, 87..89 filter gradient of any geometry, 90 forward / backward-data and strided
  * forward, 92..94 forward / backward-data of layers of few tiles; 100..106 the bf16 filter gradient over images
  * that streams its operands into LDS; 110..112 the products of the dense shard in 8 bits,
- * 113 its forward product of few results), `splitk` > 0 forces the
+ * 113 its forward product of few results, 114 its backward pass in one launch), `splitk` > 0 forces the
  * split count of the reduction (clamped to the number of reduction steps), `flags` is a set of
  * OWT_FORCE_* bits.  While an override is active, tuned and cached plans are ignored.  The three
  * values are stored atomically, but a launch that runs concurrently with this call may see the old

@@ -1,18 +1,19 @@
-// The fully-connected column shard in 8 bits: entry points of q8gemm.hpp and q8prep.hpp.
+// The fully-connected column shard in 8 bits: entry points of q8gemm.hpp, q8prep.hpp, q8few.hpp and q8fewbwd.hpp.
 #include <cmath>
 #include <initializer_list>
 
 #include "owt_host.hpp"
 #include "q8.hpp"
 #include "q8few.hpp"
+#include "q8fewbwd.hpp"
 #include "q8gemm.hpp"
 #include "q8prep.hpp"
 
 namespace owt {
 
-// Tiles of the products, 256 x 256, 128 x 128 and 64 x 64 (owt_test_force_variant: 110.. name these), and the forward product's kernel for
-// few results (113).
-constexpr int kNumQ8Tiles = 3, kQ8FirstTile = 110, kQ8Few = 3;
+// Tiles of the products, 256 x 256, 128 x 128 and 64 x 64 (owt_test_force_variant: 110.. name these), the forward product's kernel for few
+// results (113) and the backward pass in one launch (114).
+constexpr int kNumQ8Tiles = 3, kQ8FirstTile = 110, kQ8Few = 3, kQ8FewBwd = 4;
 // What a work-group takes: `start` for its beginning and end, `step` for a step on a quiet chip, `busy` where 128 or more run (256 x 256:
 // all 256; the chip is then bound by its power).  us, fitted to 20 products of 1 x 1024 -> 1024 to 8192 x 4096 -> 8192 with every tile and split.
 struct Q8Tile { int bm, bn; float start, step, busy; };
@@ -63,12 +64,12 @@ static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
 }
 
 // Both backward products in one launch of the same tile: the two tiles that have one.  0: apart they take less.
-static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long O, int dx_steps, int dw_steps)
+static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long O, int dx_steps, int dw_steps, float &least)
 {
     const int want = forced_tile() - kQ8FirstTile;
     if (forced_split() > 0) return 0;
     int best = 0;
-    float least = dx.us + dw.us;
+    least = dx.us + dw.us;
     for (int t = 1; t < kNumQ8Tiles; t++) {
         if (want >= 0 && want < kNumQ8Tiles && t != want) continue;
         const Q8Tile &q = kQ8Tiles[t];
@@ -79,6 +80,23 @@ static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long
         if (us < least) { least = us; best = t; }
     }
     return best;
+}
+
+// The whole backward pass in one launch (q8fewbwd.hpp), where that takes less than the preparation and the products.  us, fitted to both sides of
+// 65 shapes from 1 x 512 -> 512 to 64 x 9216 -> 9216 in both types; the choice then takes 0.5 % longer than the faster side on average.
+// (This and the rest, fp32: 128 rows of 512 -> 128 7.0 and 14.9, of 9216 -> 512 19.0 and 26.9, 256 rows of 4096 -> 4096 88 and 78, 8192 of
+// 512 -> 125 90 and 45.)
+static bool q8_few_bwd_is(const Q8Plan &dx, const Q8Plan &dw, int pair_or_0, float pair_us, long N, long I, long O, bool bf16)
+{
+    const int want = forced_tile() - kQ8FirstTile;
+    if (want >= 0 || forced_split() > 0) return want == kQ8FewBwd;
+    const float products = pair_or_0 ? pair_us : dx.us + dw.us;
+    const float rest = 11.f + products + (3.f * (float)(N + O) * (float)I + (float)(bf16 ? 14 : 20) * (float)N * (float)O) / 7e6f;
+    const float its = (float)((I + 127) / 128), tx = its * (float)((N + 31) / 32), tw = its * (float)((O + 31) / 32);       // work-groups
+    const float sx = (float)((O + 15) / 16), sw = (float)((N + 15) / 16), part = bf16 ? 0.65f : 1.f;                        // steps
+    const float longest = 2.5f + 0.65f * fmaxf(part * ceilf(sx / 4.f), ceilf(sw / 4.f));
+    const float all = (tx + tw) * 2.5f / 768.f + (part * tx * sx + tw * sw) * 0.45f / 1024.f;
+    return 3.f + fmaxf(longest, all + 0.4f * longest) < rest;
 }
 
 static size_t partial_bytes(const Q8Plan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
@@ -141,6 +159,7 @@ static owt_status need_ws(const void *ws, size_t have, size_t need)
 // The backward pass's scratch, laid out in order; `take` returns the offset of each part.
 struct Q8BwdLayout {
     int nk, ok, strips, strip_rows, planes, pair;
+    bool few;                           // one launch, which uses none of this
     Q8Plan dw, dx;
     size_t colsum, colmax, rowmax, cexp, rexp, aw, ax, bw, bx, partial, total;
     Q8BwdLayout(int N, int I, int O, bool bf16)
@@ -158,7 +177,9 @@ struct Q8BwdLayout {
         strips = (int)((N + rows - 1) / rows);
         dw = q8_plan(O, I, 2 * nk, false);
         dx = q8_plan(N, I, planes * ok, false);
-        pair = q8_pair_tile(dx, dw, N, I, O, planes * ok, 2 * nk);
+        float pair_us = 0.f;
+        pair = q8_pair_tile(dx, dw, N, I, O, planes * ok, 2 * nk, pair_us);
+        few = q8_few_bwd_is(dx, dw, pair, pair_us, N, I, O, bf16);
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
         colsum = take((size_t)strips * O * 4);
@@ -245,6 +266,20 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     OWT_TRY(need_ws(ws, ws_bytes, l.total));
     hipStream_t s = (hipStream_t)hip_stream;
     char *at = (char *)ws;
+    if (l.few) {
+        Q8FewBwdParams f = {dy, (d->flags & OWT_RELU) ? y_or_null : nullptr, xscale, wscale, xq, wq, d->N, d->I, ol, q8_pitch(d->I), alpha, beta,
+                            dx_partial_or_null, dw, dbias_or_null, 0, 0};
+        const long its = (d->I + 127) / 128;
+        const long tw = (ol + 31) / 32 * its, tx = want_dx ? (d->N + 31) / 32 * its : 0;
+        if (tw > 0x3fffffffL || tx > 0x3fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+        f.tiles_w = (int)tw; f.tiles_x = (int)tx;
+        const dim3 grid((unsigned)((tx ? owt_split_major_grid(f.tiles_x, 1) : 0) + owt_split_major_grid(f.tiles_w, 1)));
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, f); };
+        if (bf16) { if (f.y) go(q8_few_bwd_kernel<bf16_t, true>); else go(q8_few_bwd_kernel<bf16_t, false>); }
+        else if (f.y) go(q8_few_bwd_kernel<float, true>); else go(q8_few_bwd_kernel<float, false>);
+        const hipError_t e = hipGetLastError();
+        return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+    }
 
     Q8PrepParams q;
     memset(&q, 0, sizeof(q));

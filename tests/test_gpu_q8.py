@@ -458,3 +458,51 @@ def test_on_a_stream_of_its_own_and_in_a_graph():
         torch.cuda.synchronize()
         for a, b in zip((y, dx, dw, db), want):
             np.testing.assert_array_equal(to_host(a), b)
+
+
+# The pass in one launch splits dz times its scale in three bf16 parts (all 24 bits; two, 16 bits, for dx in bf16) and adds 16 terms of a part an
+# instruction, 3 / 16 (2 / 16) of a rounding for a term: check_backward's bounds, of two halves and 2 / 8 (one half, 1 / 8), hold for it as well.
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("N,I,O", [(1, 1, 1), (2, 125, 33), (16, 129, 512), (17, 300, 64), (63, 128, 65), (65, 1000, 31), (128, 700, 125), (300, 257, 190),
+                                   (40, 70, 2999)])
+def test_the_backward_kernel_of_few_results(N, I, O, dt):
+    say("case few, backward", N, I, O, dt)
+    with force(114):
+        s = Shard(N, I, O, dt)
+        s.y[0] = 0.0
+        s.y[:, -1] = 0.0
+        s.check_backward(1.0 / N, 0.0)
+        Shard(N, I, O, dt, relu=False).check_backward(0.5, -0.25, dx=N % 2 == 0, db=N % 3 == 0)
+
+
+@pytest.mark.parametrize("tile", [111, 112])
+def test_both_backward_products_in_one_launch(tile):
+    say("case pair", tile)
+    with force(tile):
+        for N, I, O in ((1, 1, 1), (300, 700, 520), (70, 1300, 33), (3, 260, 300)):
+            Shard(N, I, O, "bf16").check_backward(1.0, 0.5)
+            Shard(N, I, O, "f32").check_backward()
+
+
+def test_the_backward_kernel_of_few_results_keeps_what_is_not_finite_and_what_is_small():
+    m = owt()
+    with force(114):
+        s = Shard(70, 100, 90, "f32")
+        s.y[:] = 1.0
+        s.y[3, 5] = 0.0
+        s.dy[3, 5] = np.inf
+        s.check_backward()
+        s.dy[10, 20] = np.inf
+        gx, gw, gb = s.backward(1.0, 0.0)
+        assert not np.isfinite(gx[10]).any() and not np.isfinite(gw[20]).any() and gb[20] == np.inf
+        assert np.isfinite(np.delete(gx, 10, 0)).all() and np.isfinite(np.delete(gw, 20, 0)).all()
+        s = Shard(70, 100, 90, "f32", relu=False)
+        s.dy *= np.float32(2.0 ** -60)                              # no row is helped by a power of two of its own
+        s.check_backward()
+        # an empty batch
+        dw, db, d = torch.ones((3, 40), device="cuda"), torch.ones(3, device="cuda"), m.fc_desc(0, 40, 3, 1)
+        wq, ws = torch.ones((3, 128), device="cuda", dtype=torch.int8), torch.ones(3, device="cuda")
+        none = torch.empty(16, device="cuda")
+        m.owt_fc_shard_q8_bwd(d, none, none, wq, ws, None, none, 1.0, 0.5, None, dw, db, workspace(m.owt_fc_shard_q8_workspace_bytes(d, m.OWT_PASS_BWD_DATA)))
+        torch.cuda.synchronize()
+        assert (to_host(dw) == 0.5).all() and (to_host(db) == 0.5).all()
