@@ -63,13 +63,13 @@ static Q8Plan q8_plan(long M, long N, int ksteps, bool forward)
     return best;
 }
 
-// Both backward products in one launch of the same tile: the two tiles that have one.  0: apart they take less.
-static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long O, int dx_steps, int dw_steps, float &least)
+// Both backward products in one launch of the same tile: the two tiles that have one.  0: apart they take less (`least` on entry; it
+// leaves as what the choice takes).
+static int q8_pair_tile(long N, long I, long O, int dx_steps, int dw_steps, float &least)
 {
     const int want = forced_tile() - kQ8FirstTile;
     if (forced_split() > 0) return 0;
     int best = 0;
-    least = dx.us + dw.us;
     for (int t = 1; t < kNumQ8Tiles; t++) {
         if (want >= 0 && want < kNumQ8Tiles && t != want) continue;
         const Q8Tile &q = kQ8Tiles[t];
@@ -83,19 +83,19 @@ static int q8_pair_tile(const Q8Plan &dx, const Q8Plan &dw, long N, long I, long
 }
 
 // The whole backward pass in one launch (q8fewbwd.hpp), where that takes less than the preparation and the products.  us, fitted to both sides of
-// 65 shapes from 1 x 512 -> 512 to 64 x 9216 -> 9216 in both types; the choice then takes 0.5 % longer than the faster side on average.
-// (This and the rest, fp32: 128 rows of 512 -> 128 7.0 and 14.9, of 9216 -> 512 19.0 and 26.9, 256 rows of 4096 -> 4096 88 and 78, 8192 of
-// 512 -> 125 90 and 45.)
-static bool q8_few_bwd_is(const Q8Plan &dx, const Q8Plan &dw, int pair_or_0, float pair_us, long N, long I, long O, bool bf16)
+// 65 shapes from 1 x 512 -> 512 to 64 x 9216 -> 9216 in both types, with dx and without; the choice then takes 0.5 % longer than the faster side
+// on average.  (This and the rest, fp32: 128 rows of 512 -> 128 7.0 and 14.9, of 9216 -> 512 19.0 and 26.9, 256 rows of 4096 -> 4096 88 and 78,
+// 8192 of 512 -> 125 90 and 45.)
+static bool q8_few_bwd_is(float products, bool with_dx, long N, long I, long O, bool bf16)
 {
     const int want = forced_tile() - kQ8FirstTile;
     if (want >= 0 || forced_split() > 0) return want == kQ8FewBwd;
-    const float products = pair_or_0 ? pair_us : dx.us + dw.us;
-    const float rest = 11.f + products + (3.f * (float)(N + O) * (float)I + (float)(bf16 ? 14 : 20) * (float)N * (float)O) / 7e6f;
-    const float its = (float)((I + 127) / 128), tx = its * (float)((N + 31) / 32), tw = its * (float)((O + 31) / 32);       // work-groups
-    const float sx = (float)((O + 15) / 16), sw = (float)((N + 15) / 16), part = bf16 ? 0.65f : 1.f;                        // steps
-    const float longest = 2.5f + 0.65f * fmaxf(part * ceilf(sx / 4.f), ceilf(sw / 4.f));
-    const float all = (tx + tw) * 2.5f / 768.f + (part * tx * sx + tw * sw) * 0.45f / 1024.f;
+    const float dz = (float)(bf16 ? 14 : 20) * (float)N * (float)O, x = 3.f * (float)N * (float)I, w = 3.f * (float)O * (float)I;    // bytes of the preparation
+    const float rest = products + (with_dx ? 11.f + (dz + x + w) / 7e6f : 6.f + (dz + x) / 5e6f);
+    const float its = (float)((I + 127) / 128), tx = with_dx ? its * (float)((N + 31) / 32) : 0.f, tw = its * (float)((O + 31) / 32);   // work-groups
+    const float part = bf16 ? 0.65f : 1.f, sx = part * (float)((O + 15) / 16), sw = (float)((N + 15) / 16);                         // steps
+    const float longest = 2.5f + 0.65f * fmaxf(with_dx ? sx / 4.f : 0.f, ceilf(sw / 4.f));
+    const float all = (tx + tw) * 2.5f / 768.f + (tx * sx + tw * sw) * 0.45f / 1024.f;
     return 3.f + fmaxf(longest, all + 0.4f * longest) < rest;
 }
 
@@ -159,7 +159,7 @@ static owt_status need_ws(const void *ws, size_t have, size_t need)
 // The backward pass's scratch, laid out in order; `take` returns the offset of each part.
 struct Q8BwdLayout {
     int nk, ok, strips, strip_rows, planes, pair;
-    bool few;                           // one launch, which uses none of this
+    float both_us;                      // both products
     Q8Plan dw, dx;
     size_t colsum, colmax, rowmax, cexp, rexp, aw, ax, bw, bx, partial, total;
     Q8BwdLayout(int N, int I, int O, bool bf16)
@@ -177,9 +177,8 @@ struct Q8BwdLayout {
         strips = (int)((N + rows - 1) / rows);
         dw = q8_plan(O, I, 2 * nk, false);
         dx = q8_plan(N, I, planes * ok, false);
-        float pair_us = 0.f;
-        pair = q8_pair_tile(dx, dw, N, I, O, planes * ok, 2 * nk, pair_us);
-        few = q8_few_bwd_is(dx, dw, pair, pair_us, N, I, O, bf16);
+        both_us = dx.us + dw.us;
+        pair = q8_pair_tile(N, I, O, planes * ok, 2 * nk, both_us);
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
         colsum = take((size_t)strips * O * 4);
@@ -266,7 +265,7 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     OWT_TRY(need_ws(ws, ws_bytes, l.total));
     hipStream_t s = (hipStream_t)hip_stream;
     char *at = (char *)ws;
-    if (l.few) {
+    if (q8_few_bwd_is(want_dx ? l.both_us : l.dw.us, want_dx, d->N, d->I, ol, bf16)) {
         Q8FewBwdParams f = {dy, (d->flags & OWT_RELU) ? y_or_null : nullptr, xscale, wscale, xq, wq, d->N, d->I, ol, q8_pitch(d->I), alpha, beta,
                             dx_partial_or_null, dw, dbias_or_null, 0, 0};
         const long its = (d->I + 127) / 128;

@@ -47,9 +47,9 @@ __global__ void __launch_bounds__(1024) q8_few_kernel(const Q8GemmParams p)
         const unsigned char *ap = q8_uniform(ag + at), *bp = q8_uniform(bg + at);
         const unsigned dst = __builtin_amdgcn_readfirstlane(to + (i & 1) * STAGE);
         q8_load_lds(asrc[0], ap, dst);
-        q8_load_lds(asrc[1], ap, dst + 1024);
-        q8_load_lds(bsrc[0], bp, dst + 2048);
-        q8_load_lds(bsrc[1], bp, dst + 3072);
+        q8_load_lds(asrc[1], ap, dst + 1 * 1024);
+        q8_load_lds(bsrc[0], bp, dst + 2 * 1024);
+        q8_load_lds(bsrc[1], bp, dst + 3 * 1024);
     };
     const int steps = (p.ksteps - wave + WAVES - 1) / WAVES;            // of this wavefront
     const int fr = lane % 16 * 128, sw = (lane % 16 >> 1) & 7, part = lane / 16;
