@@ -311,8 +311,8 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
  *     dw[o][i] = alpha * sum_n dz[n][o] * xscale[n] * xq[n][i] + beta * dw;   dbias[o] = alpha * sum_n dz[n][o] + beta * dbias   (NULL to skip)
  * dy, y [N][O_local], dx_partial [N][I] in the descriptor's dtype; dw [O_local][I] (dense, no pitch) and dbias fp32.
  * dz times its scale is multiplied as the sum of two f16 values under a power of two for each row of a result, which hold 22 bits of all
- * that is within 2^-16 of the row's largest such value, and 2^-39 of the largest below that; one f16 value (11 bits) for dx in bf16.
- * Where there is little to multiply it is the sum of three bf16 values, which hold all 24 bits; two (16 bits) for dx in bf16.
+ * that is within 2^-16 of the row's largest such value, and 2^-39 of the largest below that, whatever dx is stored in.
+ * Where there is little to multiply it is the sum of three bf16 values, which hold all 24 bits.
  * ws: owt_fc_shard_q8_workspace_bytes of OWT_PASS_BWD_DATA (one figure for the whole pass, whichever kernels serve it), about 2 to 4 bytes
  * for every value of xq and wq and 2 to 8 for every value of dz. */
 owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,

@@ -24,9 +24,11 @@ template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, 
     const dim3 grid((unsigned)owt_split_major_grid(p.tiles, p.splits));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p); };
     if (t == 0) {
+        // two planes: step by step where a sum is of four pairs or fewer (us, by steps and by pairs: dx of 8192 x 9216 from 64 outputs 69 and 72,
+        // from 256 107 and 109, from 512 166 and 164; dw of 8192 x 4096 -> 4096 464 and 432)
         bool paired = false;
         if constexpr (std::is_same<Op, Q8Half>::value) {
-            paired = p.planes == 2;
+            paired = p.ksteps_per_split > 8;
             if (paired) go(q8gemm_kernel<Op, 2, 2, 4, 4, 5, true, 1>);
         }
         if (!paired) go(q8gemm_kernel<Op, 2, 2, 4, 4, 2, false, 1>);
@@ -83,14 +85,14 @@ static int q8_pair_tile(long N, long I, long O, int dx_steps, int dw_steps, floa
 }
 
 // The whole backward pass in one launch (q8fewbwd.hpp), where that takes less than the preparation and the products.  us, fitted to both sides of
-// 65 shapes from 1 x 512 -> 512 to 64 x 9216 -> 9216 in both types, with dx and without; the choice then takes 0.5 % longer than the faster side
-// on average.  (This and the rest, fp32: 128 rows of 512 -> 128 7.0 and 14.9, of 9216 -> 512 19.0 and 26.9, 256 rows of 4096 -> 4096 88 and 78,
+// 65 shapes from 1 x 512 -> 512 to 64 x 9216 -> 9216 in both types, with dx and without; the choice then takes 0.5 % (bf16 0.8 %) longer than the
+// faster side on average.  (This and the rest, fp32: 128 rows of 512 -> 128 7.0 and 14.9, of 9216 -> 512 19.0 and 26.9, 256 rows of 4096 -> 4096 88 and 78,
 // 8192 of 512 -> 125 90 and 45.)
 static bool q8_few_bwd_is(float products, bool with_dx, long N, long I, long O, bool bf16)
 {
     const int want = forced_tile() - kQ8FirstTile;
     if (want >= 0 || forced_split() > 0) return want == kQ8FewBwd;
-    const float dz = (float)(bf16 ? 14 : 20) * (float)N * (float)O, x = 3.f * (float)N * (float)I, w = 3.f * (float)O * (float)I;    // bytes of the preparation
+    const float dz = (float)(bf16 ? 16 : 20) * (float)N * (float)O, x = 3.f * (float)N * (float)I, w = 3.f * (float)O * (float)I;    // bytes of the preparation
     const float rest = products + (with_dx ? 11.f + (dz + x + w) / 7e6f : 6.f + (dz + x) / 5e6f);
     const float its = (float)((I + 127) / 128), tx = with_dx ? its * (float)((N + 31) / 32) : 0.f, tw = its * (float)((O + 31) / 32);   // work-groups
     const float part = bf16 ? 0.65f : 1.f, sx = part * (float)((O + 15) / 16), sw = (float)((N + 15) / 16);                         // steps
@@ -158,15 +160,14 @@ static owt_status need_ws(const void *ws, size_t have, size_t need)
 
 // The backward pass's scratch, laid out in order; `take` returns the offset of each part.
 struct Q8BwdLayout {
-    int nk, ok, strips, strip_rows, planes, pair;
+    int nk, ok, strips, strip_rows, pair;
     float both_us;                      // both products
     Q8Plan dw, dx;
     size_t colsum, colmax, rowmax, cexp, rexp, aw, ax, bw, bx, partial, total;
-    Q8BwdLayout(int N, int I, int O, bool bf16)
+    Q8BwdLayout(int N, int I, int O)
     {
         nk = N > 0 ? (N + 63) / 64 : 1;
         ok = (O + 63) / 64;
-        planes = bf16 ? 1 : 2;
         // strips: enough parts of 64 columns for the chip, no more than 64 to add up, and 64 rows or more each
         long want = (2048 + ok - 1) / ok;
         want = want > 64 ? 64 : want;
@@ -176,9 +177,9 @@ struct Q8BwdLayout {
         strip_rows = (int)rows;
         strips = (int)((N + rows - 1) / rows);
         dw = q8_plan(O, I, 2 * nk, false);
-        dx = q8_plan(N, I, planes * ok, false);
+        dx = q8_plan(N, I, 2 * ok, false);
         both_us = dx.us + dw.us;
-        pair = q8_pair_tile(N, I, O, planes * ok, 2 * nk, both_us);
+        pair = q8_pair_tile(N, I, O, 2 * ok, 2 * nk, both_us);
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
         colsum = take((size_t)strips * O * 4);
@@ -187,7 +188,7 @@ struct Q8BwdLayout {
         cexp = take((size_t)O * 4);
         rexp = take((size_t)N * 4);
         aw = take((size_t)O * nk * 256);
-        ax = take((size_t)N * ok * 128 * planes);
+        ax = take((size_t)N * ok * 256);
         bw = take((size_t)I * nk * 128);
         bx = take((size_t)I * ok * 128);
         const size_t a = partial_bytes(dw, O, I), b = partial_bytes(dx, N, I);
@@ -213,7 +214,7 @@ size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass)
         const int ks = (int)(q8_pitch(d->I) / 128);
         return partial_bytes(q8_plan(d->N, ol, ks, true), d->N, ol);
     }
-    return Q8BwdLayout(d->N, d->I, ol, d->dtype == OWT_BF16).total;
+    return Q8BwdLayout(d->N, d->I, ol).total;
 }
 
 owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
@@ -261,7 +262,7 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
         if (d->flags & OWT_RELU) OWT_TRY(need_ptr(y_or_null, "y (needed for the ReLU mask)"));
     }
     const bool bf16 = d->dtype == OWT_BF16, want_dx = dx_partial_or_null && d->N > 0;
-    const Q8BwdLayout l(d->N, d->I, ol, bf16);
+    const Q8BwdLayout l(d->N, d->I, ol);
     OWT_TRY(need_ws(ws, ws_bytes, l.total));
     hipStream_t s = (hipStream_t)hip_stream;
     char *at = (char *)ws;
@@ -299,8 +300,8 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
         hipLaunchKernelGGL(stat, dim3((unsigned)(ts + tx + tw)), dim3(256), 0, s, q);
         hipLaunchKernelGGL(halves, dim3((unsigned)tz), dim3(256), 0, s, q);
     };
-    if (bf16) { if (want_dx) prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, 1>); else prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, 0>); }
-    else { if (want_dx) prepare(q8_stat_kernel<float>, q8_prep_kernel<float, 2>); else prepare(q8_stat_kernel<float>, q8_prep_kernel<float, 0>); }
+    if (bf16) { if (want_dx) prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, true>); else prepare(q8_stat_kernel<bf16_t>, q8_prep_kernel<bf16_t, false>); }
+    else { if (want_dx) prepare(q8_stat_kernel<float>, q8_prep_kernel<float, true>); else prepare(q8_stat_kernel<float>, q8_prep_kernel<float, false>); }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
 
@@ -313,8 +314,8 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     w.d = {q.col_exp, alpha, beta};
     x = w;
     x.a = (const unsigned char *)q.ax; x.b = (const unsigned char *)q.bx;
-    x.lda = (size_t)l.ok * 128 * l.planes; x.ldb = (size_t)l.ok * 128;
-    x.M = d->N; x.ksteps = l.planes * l.ok; x.planes = l.planes;
+    x.lda = (size_t)l.ok * 256; x.ldb = (size_t)l.ok * 128;
+    x.M = d->N; x.ksteps = 2 * l.ok;
     x.out = dx_partial_or_null; x.bf16 = bf16;
     x.d = {q.row_exp, 1.f, 0.f};
     if (want_dx && l.pair) {

@@ -2,9 +2,8 @@
 //
 // The products of q8gemm.hpp want operands with consecutive k and a power of two for each row of a result, which take two launches.
 // Here both operands are read as they lie and put in order in registers.  dz times its scale is split in bf16 parts by truncation: three of
-// 8 bits are all 24 of an fp32 value, and bf16 has fp32's exponents, so that nothing needs to be known of the other values; dx in bf16 takes two
-// parts (16 bits, where the result keeps 8).  Whole numbers of 8 bits are exact in bf16.  A wavefront has 32 rows x 128 columns of a result
-// (v_mfma_f32_32x32x16_bf16): of each of a step's sixteen rows of whole numbers a lane reads the four of columns 4 (lane % 32) .., one
+// 8 bits are all 24 of an fp32 value, and bf16 has fp32's exponents, so that nothing needs to be known of the other values.  Whole numbers of 8 bits
+// are exact in bf16.  A wavefront has 32 rows x 128 columns of a result (v_mfma_f32_32x32x16_bf16): of each of a step's sixteen rows of whole numbers a lane reads the four of columns 4 (lane % 32) .., one
 // column of each of its four tiles, so that a lane's results of a row are four neighbours.  The four wavefronts of a work-group take every
 // fourth step and add up in LDS, in a fixed order.
 //
@@ -36,7 +35,7 @@ constexpr int kQ8FewBwdLds = 2 * 16 * 64 * 16 + 4 * 32 * 4;
 template <class T, bool DX, bool MASK>
 __device__ __forceinline__ void q8_few_bwd(const Q8FewBwdParams &p, int mt, int it, unsigned char *lds)
 {
-    constexpr int PLANES = DX && sizeof(T) == 2 ? 2 : 3, WAVES = 4;
+    constexpr int PARTS = 3, WAVES = 4;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5, l = lane & 31;
     const int M = DX ? p.N : p.O, K = DX ? p.O : p.N;
     const signed char *q = (DX ? p.wq : p.xq) + it * 128;
@@ -94,7 +93,7 @@ __device__ __forceinline__ void q8_few_bwd(const Q8FewBwdParams &p, int mt, int 
     q8_f32x16 acc[4] = {};
     float bias = 0.f;
     auto multiply = [&](const Raw &r, int step) __attribute__((always_inline)) {
-        uint32_t part[PLANES][8];
+        uint32_t part[PARTS][8];
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; j++) {
@@ -108,15 +107,15 @@ __device__ __forceinline__ void q8_few_bwd(const Q8FewBwdParams &p, int mt, int 
 #pragma unroll
         for (int j = 0; j < 8; j++) {
 #pragma unroll
-            for (int i = 0; i < PLANES; i++) {
+            for (int i = 0; i < PARTS; i++) {
                 part[i][j] = __float_as_uint(v[j]);
                 const float rest = v[j] - __uint_as_float(part[i][j] & 0xffff0000u);
                 v[j] = i || fabsf(v[j]) < __uint_as_float(0x7f800000u) ? rest : 0.f;    // what is not finite is its first part
             }
         }
-        q8_bf16x8 a[PLANES];
+        q8_bf16x8 a[PARTS];
 #pragma unroll
-        for (int i = 0; i < PLANES; i++) {
+        for (int i = 0; i < PARTS; i++) {
             q8_u32x4 w;
 #pragma unroll
             for (int j = 0; j < 4; j++) w[j] = __builtin_amdgcn_perm(part[i][2 * j + 1], part[i][2 * j], 0x07060302u);
@@ -132,7 +131,7 @@ __device__ __forceinline__ void q8_few_bwd(const Q8FewBwdParams &p, int mt, int 
             }
             const q8_bf16x8 b = __builtin_bit_cast(q8_bf16x8, w);
 #pragma unroll
-            for (int i = PLANES - 1; i >= 0; i--) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b, acc[t], 0, 0, 0);
+            for (int i = PARTS - 1; i >= 0; i--) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b, acc[t], 0, 0, 0);
         }
     };
     const std::integral_constant<bool, DX> near;

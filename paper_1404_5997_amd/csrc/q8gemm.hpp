@@ -171,7 +171,7 @@ __device__ __forceinline__ void q8_load_lds(unsigned off, const unsigned char *b
 // PAIRS: the steps of A go in pairs that meet the same step of B, and lds holds NS tiles of one operand, filled one by one in the order they
 // are used.  256 x 256 results take 32 KB of either operand a step, so that two stages are all that LDS holds; this way B is loaded once for a
 // pair, its fragments, read from LDS with the first plane, stay in registers for the second, and with five tiles a load has two products of
-// a step to arrive in instead of less than one (dw of 8192 x 4096 -> 4096 432 us, 466 by stages; one plane by five tiles 244 us, 231 by stages).
+// a step to arrive in instead of less than one (dw of 8192 x 4096 -> 4096 432 us, 466 by stages, which are the faster ones where sums are short).
 template <class Op, int WM, int WN, int MB, int NB, int NS, bool PAIRS>
 __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int split, unsigned char *lds)
 {

@@ -3,8 +3,8 @@
 // With dz = dy where y > 0 (or dy), the left operands are  dw: A[o][n] = dz[n][o] xs[n],  dx: A[n][o] = dz[n][o] ws[o],  the right ones the
 // whole numbers, transposed: B[i][n] = xq[n][i],  B[i][o] = wq[o][i].  Whole numbers of 8 bits are exact in f16.  A row of a left operand
 // is scaled by a power of two that takes its largest finite magnitude to [2^14, 2^15), and each value is written as h + m, two f16
-// values: that holds 22 bits of a value of 2^-16 of the row's largest and more, and 2^-39 of the largest below.  bf16 dx takes h alone (11
-// bits, where the result keeps 8).  A value that is not finite is h by itself.
+// values: that holds 22 bits of a value of 2^-16 of the row's largest and more, and 2^-39 of the largest below.  (bf16 dx as well: of h alone
+// its sums are off by 2^-12 of their terms, which is more than the result's own rounding where they cancel.)  A value that is not finite is h by itself.
 //
 // First launch: the whole numbers are turned, and dz is read once for the bias gradient's sums and the largest magnitudes of columns (times
 // xs) and rows (times ws), in parts of 64 columns x a strip of rows.  Second launch: the left operands, 64 x 64 values a work-group, the
@@ -33,7 +33,7 @@ struct Q8PrepParams {
     float *colmax;                      // [strips][O]
     float *rowmax;                      // [ceil(O/64)][N]
     int *col_exp, *row_exp;             // [O], [N]
-    _Float16 *aw, *ax, *bw, *bx;        // dw: [O][nk][2][64], dx: [N][ok][planes][64]; [I][nk][64], [I][ok][64]
+    _Float16 *aw, *ax, *bw, *bx;        // dw: [O][nk][2][64], dx: [N][ok][2][64]; [I][nk][64], [I][ok][64]
     int nk, ok;                         // steps of 64 rows (tokens), of 64 outputs
     int tiles_s, tiles_x;               // work-groups of the first launch: statistics, then xq's tiles, then wq's
 };
@@ -190,8 +190,8 @@ template <class T> __global__ void __launch_bounds__(256) q8_stat_kernel(const Q
     }
 }
 
-// A 64 x 64 tile of dz.  DX: planes of dx's operand, 0 = none.
-template <class T, int DX, int HOW> __device__ __forceinline__ void q8_split(const Q8PrepParams &p, uint32_t *tile, int *ce, int *re)
+// A 64 x 64 tile of dz.  DX: dx's operand, too.
+template <class T, bool DX, int HOW> __device__ __forceinline__ void q8_split(const Q8PrepParams &p, uint32_t *tile, int *ce, int *re)
 {
     constexpr int V = Piece<T>::V, LPR = 64 / V, RPP = 256 / LPR, PASSES = 64 / RPP;       // lanes a row, rows a pass
     const int tid = threadIdx.x, nt = blockIdx.x / p.ok, ot = blockIdx.x % p.ok, n0 = nt * 64, o0 = ot * 64;
@@ -251,13 +251,13 @@ template <class T, int DX, int HOW> __device__ __forceinline__ void q8_split(con
                 h[i] = __builtin_amdgcn_perm(both[2 * i + 1], both[2 * i], 0x05040100u);
                 m[i] = __builtin_amdgcn_perm(both[2 * i + 1], both[2 * i], 0x07060302u);
             }
-            _Float16 *at = p.ax + ((size_t)n * p.ok + ot) * (DX * 64) + lc * V;
+            _Float16 *at = p.ax + ((size_t)n * p.ok + ot) * 128 + lc * V;
             if (V == 8) {
                 *(uint4 *)at = make_uint4(h[0], h[1], h[V / 2 - 2], h[V / 2 - 1]);
-                if (DX == 2) *(uint4 *)(at + 64) = make_uint4(m[0], m[1], m[V / 2 - 2], m[V / 2 - 1]);
+                *(uint4 *)(at + 64) = make_uint4(m[0], m[1], m[V / 2 - 2], m[V / 2 - 1]);
             } else {
                 *(uint2 *)at = make_uint2(h[0], h[1]);
-                if (DX == 2) *(uint2 *)(at + 64) = make_uint2(m[0], m[1]);
+                *(uint2 *)(at + 64) = make_uint2(m[0], m[1]);
             }
         }
     }
@@ -281,7 +281,7 @@ template <class T, int DX, int HOW> __device__ __forceinline__ void q8_split(con
     }
 }
 
-template <class T, int DX> __global__ void __launch_bounds__(256) q8_prep_kernel(const Q8PrepParams p)
+template <class T, bool DX> __global__ void __launch_bounds__(256) q8_prep_kernel(const Q8PrepParams p)
 {
     __shared__ uint32_t tile[64 * 65];              // [n][o], both halves of a value in a word
     __shared__ int ce[64], re[64];
