@@ -101,11 +101,9 @@ def _ptr(t):
     """Device pointer of a torch tensor (or a raw int / None passed through)."""
     if t is None:
         return None
-    try:
-        dense = t.is_contiguous()
-    except AttributeError:
+    if isinstance(t, int):
         return t
-    if not dense:
+    if not t.is_contiguous():
         raise ValueError("owt takes dense row-major tensors")
     return t.data_ptr()
 
