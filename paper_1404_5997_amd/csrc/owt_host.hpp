@@ -15,6 +15,9 @@ void clear_error();
 int forced_tile();          // what owt_test_force_variant set, or -1
 int forced_split();
 
+// A launch counts its threads in 32 bits (owt_split_major_grid rounds up to eight work-groups).
+inline bool groups_fit(long groups, int threads) { return groups <= (1L << 32) / threads - 8; }
+
 inline bool aligned16(const void *p) { return (((uintptr_t)p) & 15u) == 0; }
 
 // Tile shapes the implicit-GEMM kernel is instantiated for.

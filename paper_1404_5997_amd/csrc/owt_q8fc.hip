@@ -103,22 +103,28 @@ static bool q8_few_bwd_is(float products, bool with_dx, long N, long I, long O, 
 
 static size_t partial_bytes(const Q8Plan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
 
+// Whether a launch holds the tiles of a product.
+static bool product_fits(const Q8Plan &pl, long M, long N)
+{
+    const Q8Tile &q = kQ8Tiles[pl.tile];
+    return groups_fit(((M + q.bm - 1) / q.bm) * ((N + q.bn - 1) / q.bn) * pl.splits, 256);
+}
+static owt_status too_many_groups() { return fail(OWT_EUNSUPPORTED, "more work-groups than a launch holds"); }
+
 // Numbers the tiles of a product.
-static bool lay_tiles(Q8GemmParams &p, const Q8Plan &pl)
+static void lay_tiles(Q8GemmParams &p, const Q8Plan &pl)
 {
     const Q8Tile &q = kQ8Tiles[pl.tile];
     p.tiles_n = (p.N + q.bn - 1) / q.bn;
-    const long tiles = (long)p.tiles_n * ((p.M + q.bm - 1) / q.bm);
-    p.tiles = (int)tiles;
+    p.tiles = p.tiles_n * ((p.M + q.bm - 1) / q.bm);
     p.splits = pl.splits;
     p.big = (size_t)p.M * p.N * (p.bf16 ? 2 : 4) > (32u << 20);
     p.ksteps_per_split = ((p.ksteps / p.planes + pl.splits - 1) / pl.splits) * p.planes;
-    return tiles * pl.splits <= 0x3fffffffL;
 }
 
 template <class Op> static owt_status run_product(Q8GemmParams p, const Q8Plan &pl, void *partial, hipStream_t s)
 {
-    if (!lay_tiles(p, pl)) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+    lay_tiles(p, pl);
     p.partial = partial;
     hipError_t e = launch_tile<Op>(pl.tile, p, s);
     if (e == hipSuccess && pl.splits > 1) {
@@ -238,12 +244,13 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
     p.f = {xscale, wscale, (d->flags & OWT_BIAS) ? bias : nullptr, (d->flags & OWT_RELU) ? 0.f : -INFINITY};
     if (pl.tile == kQ8Few) {
         const long tiles = (long)((p.M + 15) / 16) * ((p.N + 15) / 16);
-        if (tiles > 0x3fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+        if (!groups_fit(tiles, 1024)) return too_many_groups();
         p.tiles = (int)tiles;
         hipLaunchKernelGGL(q8_few_kernel, dim3((unsigned)owt_split_major_grid(p.tiles, 1)), dim3(1024), 0, (hipStream_t)hip_stream, p);
         const hipError_t e = hipGetLastError();
         return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
     }
+    if (!product_fits(pl, d->N, ol)) return too_many_groups();
     return run_product<Q8Int>(p, pl, ws, (hipStream_t)hip_stream);
 }
 
@@ -271,7 +278,7 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
                             dx_partial_or_null, dw, dbias_or_null, 0, 0};
         const long its = (d->I + 127) / 128;
         const long tw = (ol + 31) / 32 * its, tx = want_dx ? (d->N + 31) / 32 * its : 0;
-        if (tw > 0x3fffffffL || tx > 0x3fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+        if (!groups_fit(tw + tx + 8, 256)) return too_many_groups();
         f.tiles_w = (int)tw; f.tiles_x = (int)tx;
         const dim3 grid((unsigned)((tx ? owt_split_major_grid(f.tiles_x, 1) : 0) + owt_split_major_grid(f.tiles_w, 1)));
         auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, f); };
@@ -294,7 +301,10 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     q.aw = (_Float16 *)(at + l.aw); q.ax = (_Float16 *)(at + l.ax); q.bw = (_Float16 *)(at + l.bw); q.bx = (_Float16 *)(at + l.bx);
     q.nk = l.nk; q.ok = l.ok;
     const long its = (d->I + 127) / 128, tz = (long)l.nk * l.ok, ts = (long)l.ok * l.strips, tx = its * l.nk, tw = want_dx ? its * l.ok : 0;
-    if (ts + tx + tw > 0x7fffffffL || tz > 0x7fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 tiles of 64 x 64 values");
+    const bool together = want_dx && l.pair;
+    const Q8Plan pair{l.pair, 1, 0.f}, &plan_w = together ? pair : l.dw, &plan_x = together ? pair : l.dx;
+    if (!groups_fit(ts + tx + tw, 256) || !groups_fit(tz, 256) || !product_fits(plan_w, ol, d->I) || (want_dx && !product_fits(plan_x, d->N, d->I)))
+        return too_many_groups();
     q.tiles_s = (int)ts; q.tiles_x = (int)tx;
     auto prepare = [&](auto stat, auto halves) {
         hipLaunchKernelGGL(stat, dim3((unsigned)(ts + tx + tw)), dim3(256), 0, s, q);
@@ -318,9 +328,9 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
     x.M = d->N; x.ksteps = 2 * l.ok;
     x.out = dx_partial_or_null; x.bf16 = bf16;
     x.d = {q.row_exp, 1.f, 0.f};
-    if (want_dx && l.pair) {
-        const Q8Plan pl{l.pair, 1, 0.f};
-        if (!lay_tiles(w, pl) || !lay_tiles(x, pl)) return fail(OWT_EUNSUPPORTED, "more than 2^30 tiles");
+    if (together) {
+        lay_tiles(w, pair);
+        lay_tiles(x, pair);
         const dim3 grid((unsigned)(owt_split_major_grid(x.tiles, 1) + owt_split_major_grid(w.tiles, 1)));
         const bool dx_first = x.ksteps >= w.ksteps;
         const Q8GemmParams &p0 = dx_first ? x : w, &p1 = dx_first ? w : x;

@@ -7,17 +7,38 @@
 
 namespace owt {
 
-// A row of n pieces: threads a row and pieces a thread.  Rows of up to 64 threads need no barrier, and short ones share a wavefront.
 // more than an eighth of the 256 MB behind the L2 caches
 template <class T> static bool big(int rows, int cols) { return (size_t)rows * cols * sizeof(T) > (32u << 20); }
 
+// A launch counts its threads in 32 bits: rows that take more work-groups than half of that go in several launches.
+constexpr long kLaunchThreads = 1L << 31;
+template <class F> static void launches_of(int rows, long most, F f)
+{
+    const int each = (int)(most < rows ? most : rows);
+    for (long first = 0; first < rows; first += each) f((size_t)first, (int)(rows - first < each ? rows - first : each));
+}
+template <class T> static Q8RowParams rows_from(Q8RowParams p, size_t first, int rows)
+{
+    p.x = (const T *)p.x + first * p.cols;
+    if (p.res) p.res = (const T *)p.res + first * p.cols;
+    if (p.h) p.h = (T *)p.h + first * p.cols;
+    p.q += first * p.pitch;
+    p.scale += first;
+    if (p.rstd) p.rstd += first;
+    p.rows = rows;
+    return p;
+}
+
+// A row of n pieces: threads a row and pieces a thread.  Rows of up to 64 threads need no barrier, and short ones share a wavefront.
 template <class T, bool NORM, bool RES, bool BIG>
 static void launch_rows_as(const Q8RowParams &p, hipStream_t s)
 {
     const long n = (long)(p.pitch / Piece<T>::V);
     auto go = [&](auto kernel, int tpr) {
         const int threads = tpr > 256 ? tpr : 256, rpw = threads / tpr;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)((p.rows + rpw - 1) / rpw)), dim3(threads), 0, s, p);
+        launches_of(p.rows, kLaunchThreads / threads * rpw, [&](size_t first, int rows) {
+            hipLaunchKernelGGL(kernel, dim3((unsigned)((rows + rpw - 1) / rpw)), dim3(threads), 0, s, rows_from<T>(p, first, rows));
+        });
     };
     if (n <= 16) go(q8_rows_kernel<T, NORM, RES, 16, 1, false, BIG>, 16);
     else if (n <= 32) go(q8_rows_kernel<T, NORM, RES, 32, 1, false, BIG>, 32);
@@ -43,8 +64,11 @@ template <class T> static void launch_unpack(const signed char *q, const float *
     int lpr = 0;
     while (lpr < 8 && (1L << lpr) < n) lpr++;
     const unsigned segs = (unsigned)((n + (1L << lpr) - 1) >> lpr), rpw = 256u >> lpr;
-    hipLaunchKernelGGL(q8_unpack_kernel<T>, dim3((unsigned)((rows + rpw - 1) / rpw) * segs), dim3(256), 0, s, q, scale, (T *)x, rows, cols,
-                       q8_pitch(cols), lpr, segs);
+    const size_t pitch = q8_pitch(cols);
+    launches_of(rows, kLaunchThreads / 256 / segs * rpw, [&](size_t first, int n_rows) {
+        hipLaunchKernelGGL(q8_unpack_kernel<T>, dim3((unsigned)((n_rows + rpw - 1) / rpw) * segs), dim3(256), 0, s, q + first * pitch, scale + first,
+                           (T *)x + first * cols, n_rows, cols, pitch, lpr, segs);
+    });
 }
 
 // Strips of rows that the backward pass sums the gain's gradient over, one in flight for each group of threads: as many as hide its loads
