@@ -369,8 +369,16 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     const int m_end = __builtin_amdgcn_readfirstlane(max(0, min(32 * MB, p.M - m0 - wm0)));     // rows of this wavefront that exist
     const unsigned char *src = mine + lane / QW * (QW * 16);
     const int *factor = rows + wm0 + lane / QW;
+    // Lanes read what others of their wavefront wrote, and write where others read.  LDS takes a wavefront's accesses in order; this keeps the
+    // compiler to that order, too, and is no instruction.
+    auto in_order = [] __attribute__((always_inline)) () {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
 #pragma unroll
     for (int i = 0; i < MB; i++) {
+        if (i > 0) in_order();
 #pragma unroll
         for (int j = 0; j < NB; j++)
 #pragma unroll
@@ -383,6 +391,7 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
                 }
                 *(q8_i32x4 *)(mine + (li * QW + ((8 * j + 2 * g + lh) ^ (li & SW))) * 16) = v;
             }
+        in_order();
         q8_how(p, p.splits > 1, [&](auto how, auto vec) __attribute__((always_inline)) {
             constexpr int HOW = decltype(how)::value;
             constexpr bool HALF = HOW == Q8_BF16 || HOW == Q8_BF16_ONCE;
