@@ -313,8 +313,9 @@ owt_status owt_fc_shard_q8_fwd(const owt_fc_desc *d, const signed char *xq, cons
  * dz times its scale is multiplied as the sum of two f16 values under a power of two for each row of a result, which hold 22 bits of all
  * that is within 2^-16 of the row's largest such value, and 2^-39 of the largest below that, whatever dx is stored in.
  * Where there is little to multiply it is the sum of three bf16 values, which hold all 24 bits.
- * ws: owt_fc_shard_q8_workspace_bytes of OWT_PASS_BWD_DATA (one figure for the whole pass, whichever kernels serve it), about 2 to 4 bytes
- * for every value of xq and wq and 2 to 8 for every value of dz. */
+ * ws: owt_fc_shard_q8_workspace_bytes of OWT_PASS_BWD_DATA (one figure for the whole pass, whichever kernels serve it, with dx or without).  With N
+ * and O_local in whole 64s it is 2 bytes for every value of xq and wq and 8 for every value of dz, a few more for what is summed over rows, and 4 for every
+ * value of dx or dw and part where the planner splits a product's sums. */
 owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, const float *xscale, const signed char *wq, const float *wscale,
                                const void *y_or_null, const void *dy, float alpha, float beta, void *dx_partial_or_null, float *dw,
                                float *dbias_or_null, void *ws, size_t ws_bytes, void *hip_stream);

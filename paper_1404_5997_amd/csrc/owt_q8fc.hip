@@ -136,6 +136,9 @@ template <class Op> static owt_status run_product(Q8GemmParams p, const Q8Plan &
 }
 
 constexpr int kQ8MaxI = 131071;         // 128 * 128 * 131071 < 2^31: no sum of products leaves 32 bits
+constexpr int kQ8MaxRows = 1 << 22;     // of x and of w
+// an operand's row, two f16 planes of kQ8MaxRows values or kQ8MaxI bytes: the last of a tile's 256 is addressed from the first with 32 bits
+static_assert(255ull * (kQ8MaxRows / 64 * 256ull) + 128 <= 0xffffffffull && kQ8MaxI < kQ8MaxRows, "offsets within a tile fit 32 bits");
 
 static owt_status check_q8_fc(const owt_fc_desc *d, int &o_local)
 {
@@ -148,7 +151,7 @@ static owt_status check_q8_fc(const owt_fc_desc *d, int &o_local)
     if (d->flags & ~(unsigned)(OWT_BIAS | OWT_RELU)) return fail(OWT_EINVAL, "unknown flag bits 0x%x", d->flags);
     o_local = d->O_total / d->workers;
     if (d->I > kQ8MaxI) return fail(OWT_EUNSUPPORTED, "more than %d inputs", kQ8MaxI);
-    if (d->N > (1 << 22) || o_local > (1 << 22)) return fail(OWT_EUNSUPPORTED, "more than 2^22 rows or columns");
+    if (d->N > kQ8MaxRows || o_local > kQ8MaxRows) return fail(OWT_EUNSUPPORTED, "more than 2^22 rows or columns");
     return OWT_OK;
 }
 static owt_status need_ptr(const void *p, const char *what)

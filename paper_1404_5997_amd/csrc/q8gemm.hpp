@@ -193,7 +193,7 @@ __device__ __forceinline__ void q8gemm_tile(const Q8GemmParams &p, int tile, int
     const int ks_beg = split * p.ksteps_per_split;
     const int nst = min(p.ksteps, ks_beg + p.ksteps_per_split) - ks_beg;
 
-    // byte offsets of this lane's pieces of a step from the tile's first row (rows of up to 2^23 bytes: the host sees to it)
+    // byte offsets of this lane's pieces of a step from the tile's first row, in 32 bits (255 rows of up to 2^24 bytes: the host sees to it)
     unsigned asrc[AI], bsrc[BI];
 #pragma unroll
     for (int i = 0; i < AI; i++) {

@@ -8,7 +8,7 @@
 //
 // First launch: the whole numbers are turned, and dz is read once for the bias gradient's sums and the largest magnitudes of columns (times
 // xs) and rows (times ws), in parts of 64 columns x a strip of rows.  Second launch: the left operands, 64 x 64 values a work-group, the
-// one of dw turned through LDS.  Both are bound by memory: 8192 x 4096 -> 4096 in bf16 moves 500 MB in 119 us.  (One
+// one of dw turned through LDS.  Both are bound by memory: 8192 x 4096 -> 4096 in bf16 moves 580 MB in 120 us.  (One
 // launch for few rows and columns, each work-group finding the magnitudes of its own: 128 x 9216 -> 512 16 us where these two take 12.)
 #pragma once
 #include <type_traits>
