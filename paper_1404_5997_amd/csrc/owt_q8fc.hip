@@ -25,7 +25,7 @@ template <class Op> static hipError_t launch_tile(int t, const Q8GemmParams &p, 
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, p); };
     if (t == 0) {
         // two planes: step by step where a sum is of four pairs or fewer (us, by steps and by pairs: dx of 8192 x 9216 from 64 outputs 69 and 72,
-        // from 256 107 and 109, from 512 166 and 164; dw of 8192 x 4096 -> 4096 464 and 432)
+        // from 256 107 and 109, from 512 166 and 164; dw of 8192 x 4096 -> 4096 466 and 432)
         bool paired = false;
         if constexpr (std::is_same<Op, Q8Half>::value) {
             paired = p.ksteps_per_split > 8;
