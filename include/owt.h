@@ -321,6 +321,64 @@ owt_status owt_fc_shard_q8_bwd(const owt_fc_desc *d, const signed char *xq, cons
                                float *dbias_or_null, void *ws, size_t ws_bytes, void *hip_stream);
 size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass);     /* (size_t)-1 on a bad descriptor */
 
+/* ---- Softmax cross-entropy on a dense shard's outputs, without the outputs ----
+ *
+ * The output layer for classes that exclude one another: beside owt_logistic_xent, which takes them one by one.  The N x O_local outputs
+ *     z[n][o] = bias[o] + sum_i x[n][i] * w[o][i],  o over this worker's columns [rank * O_local, (rank + 1) * O_local) of O_total
+ * are never stored whole: the columns are taken in pieces.  x [N][I] and w [O_local][I] in the descriptor's dtype, bias fp32, read only with
+ * OWT_BIAS (the only flag).  labels [N]: class index in the whole layer.  A row whose label is outside [0, O_total) has no class: it is padding,
+ * whatever its x holds (infinities and NaN, too) has no influence on any other row, its lse, target, loss and dx are 0.
+ * A bias of -infinity takes a class out: it adds nothing to lse and gets no gradient.  N == 0 is an empty batch.
+ * N, O_local <= 2^22 and x and w of at most 2^31-1 values (OWT_EUNSUPPORTED).
+ *
+ * bf16 operands are multiplied as they are.  fp32 ones may be multiplied as sums of two f16 values under a power of two for each row of x and of w
+ * (in the backward pass also of dz), which hold 22 bits of all that is within 2^-16 of the row's largest magnitude, and 2^-39 of the largest below that.
+ * dz meets x, for dw, as the sum of two values of 8 (bf16) or 11 bits, and w, for dx, as one in bf16: dx is rounded to bf16 itself. */
+
+/* Forward pass:  lse[n] = log sum_o exp z[n][o] (-infinity where every output is);  target[n] = z[n][label] if the label is one of this worker's
+ * columns, else -infinity;  loss[n] = lse[n] - target[n] (+infinity for a class that is taken out).  All [N] fp32.  labels may be NULL (then target and
+ * loss have to be): lse of all rows.  loss needs workers == 1; of several workers' shares owt_softmax_join makes it. */
+owt_status owt_fc_softmax_fwd(const owt_fc_desc *d, const void *x, const void *w, const float *bias, const int *labels_or_null, float *lse,
+                              float *target_or_null, float *loss_or_null, void *ws, size_t ws_bytes, void *hip_stream);
+
+/* What the workers' shares come to: lses, targets [workers][N] as their forward passes left them; lse, target, loss [N] of the whole layer of
+ * `classes` outputs.  Two floats a row and worker are all that a softmax over a divided layer has to exchange. */
+owt_status owt_softmax_join(int workers, int N, int classes, const float *lses, const float *targets, const int *labels, float *lse,
+                            float *target_or_null, float *loss_or_null, void *hip_stream);
+
+/* Backward pass, from the whole layer's lse:
+ *     dz[n][o] = weight[n] * (exp(z[n][o] - lse[n]) - [o is n's label])          (weight NULL: all ones)
+ *     dx_partial[n][i] = sum_o dz[n][o] * w[o][i]                                (this worker's addend; NULL to skip)
+ *     dw[o][i] = alpha * sum_n dz[n][o] * x[n][i] + beta * dw;   dbias[o] = alpha * sum_n dz[n][o] + beta * dbias   (NULL to skip)
+ * weight [N] fp32 is the gradient that arrives at each row's loss; alpha, beta as in owt_fc_shard_bwd; dx_partial [N][I] in the descriptor's dtype,
+ * dw [O_local][I] and dbias fp32.  The outputs are computed again. */
+owt_status owt_fc_softmax_bwd(const owt_fc_desc *d, const void *x, const void *w, const float *bias, const int *labels, const float *lse,
+                              const float *weight_or_null, float alpha, float beta, void *dx_partial_or_null, float *dw, float *dbias_or_null, void *ws,
+                              size_t ws_bytes, void *hip_stream);
+size_t owt_fc_softmax_workspace_bytes(const owt_fc_desc *d, int pass);      /* (size_t)-1 on a bad descriptor */
+
+/* ---- The norm of many gradients together, and steps that it bounds ----
+ *
+ * Lists of `count` tensors: HOST arrays of sizes (values, each may be 0) and of device pointers, read before the call returns.  Every tensor is dense
+ * and 16-byte aligned; no two of a list overlap.  A pointer of an empty tensor may be anything.  Sizes up to 2^40 (OWT_EUNSUPPORTED). */
+
+/* norm[0] = sqrt of the sum of the squares of all values of all tensors, in `dtype`.  The sum is taken in 64 bits; norm is one fp32 value on the
+ * device, 16-byte aligned, 0 for an empty list, not finite where a value is not or fp32 does not hold it.  (Of a model divided over workers: the root of the sum
+ * of the squares of their norms.) */
+owt_status owt_grad_norm(int count, const size_t *n, const void *const *g, owt_dtype dtype, float *norm, void *ws, size_t ws_bytes, void *hip_stream);
+size_t owt_grad_norm_workspace_bytes(int count, const size_t *n);           /* (size_t)-1 on bad sizes */
+
+/* out[t] = g[t] * min(1, max_norm / norm[0]) in `dtype`; out[t] may be g[t] itself, and is then not touched where nothing changes.  Where the norm is
+ * not finite out is all zeros.  max_norm > 0; infinity: no bound. */
+owt_status owt_grad_clip(int count, const size_t *n, const void *const *g, void *const *out, owt_dtype dtype, const float *norm, float max_norm,
+                         void *hip_stream);
+
+/* owt_sgd_momentum_update of many tensors with the bounded gradient f * gscale * g in the place of gscale * g, f = min(1, max_norm / (|gscale| * norm[0])):
+ *     vel := mu*vel + eps*(f*gscale*g - omega*w);   w := w + vel
+ * norm: owt_grad_norm of the g.  Where it is not finite there is no step: w, vel and the bf16 copies stay as they are. */
+owt_status owt_sgd_momentum_clipped(int count, const size_t *n, float *const *w, float *const *vel, const float *const *g, float mu, float eps,
+                                    float omega, float gscale, const float *norm, float max_norm, void *const *w_bf16_or_null, void *hip_stream);
+
 /* Message for the calling thread's most recent non-OK return ("" if none).
  * Points at thread-local static storage; valid until the thread's next call. */
 const char *owt_last_error(void);

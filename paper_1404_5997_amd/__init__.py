@@ -30,6 +30,8 @@ EXPORTS = (
     "owt_conv_bwd_filter_static", "owt_static_scratch_bytes",
     "owt_q8_pitch", "owt_q8_pack", "owt_q8_unpack", "owt_rmsnorm_q8_fwd", "owt_rmsnorm_q8_bwd", "owt_rmsnorm_q8_workspace_bytes",
     "owt_fc_shard_q8_fwd", "owt_fc_shard_q8_bwd", "owt_fc_shard_q8_workspace_bytes",
+    "owt_fc_softmax_fwd", "owt_softmax_join", "owt_fc_softmax_bwd", "owt_fc_softmax_workspace_bytes",
+    "owt_grad_norm", "owt_grad_norm_workspace_bytes", "owt_grad_clip", "owt_sgd_momentum_clipped",
 )
 
 
@@ -90,6 +92,16 @@ _lib.owt_fc_shard_q8_fwd.argtypes = [_fd, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz
 _lib.owt_fc_shard_q8_bwd.argtypes = [_fd, _vp, _vp, _vp, _vp, _vp, _vp, _f, _f, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.owt_fc_shard_q8_workspace_bytes.restype = _sz
 _lib.owt_fc_shard_q8_workspace_bytes.argtypes = [_fd, _i]
+_lib.owt_fc_softmax_fwd.argtypes = [_fd, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.owt_softmax_join.argtypes = [_i, _i, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.owt_fc_softmax_bwd.argtypes = [_fd, _vp, _vp, _vp, _vp, _vp, _vp, _f, _f, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.owt_fc_softmax_workspace_bytes.restype = _sz
+_lib.owt_fc_softmax_workspace_bytes.argtypes = [_fd, _i]
+_lib.owt_grad_norm.argtypes = [_i, _vp, _vp, _i, _vp, _vp, _sz, _vp]
+_lib.owt_grad_norm_workspace_bytes.restype = _sz
+_lib.owt_grad_norm_workspace_bytes.argtypes = [_i, _vp]
+_lib.owt_grad_clip.argtypes = [_i, _vp, _vp, _vp, _i, _vp, _f, _vp]
+_lib.owt_sgd_momentum_clipped.argtypes = [_i, _vp, _vp, _vp, _vp, _f, _f, _f, _f, _vp, _f, _vp, _vp]
 _lib.owt_last_error.restype = ctypes.c_char_p
 _lib.owt_abi_version.restype = _i
 _lib.owt_conv_plan_describe.argtypes = [_cd, _i, ctypes.c_char_p, _sz]
@@ -321,3 +333,75 @@ def owt_fc_shard_q8_bwd(desc, xq, xscale, wq, wscale, y_or_null, dy, alpha, beta
     p, n = _ws(ws)
     _check(_lib.owt_fc_shard_q8_bwd(ctypes.byref(desc), _ptr(xq), _ptr(xscale), _ptr(wq), _ptr(wscale), _ptr(y_or_null), _ptr(dy), alpha,
                                     beta, _ptr(dx_partial_or_null), _ptr(dw), _ptr(dbias_or_null), p, n, _stream(stream)))
+
+
+def owt_fc_softmax_workspace_bytes(desc, pass_):
+    n = _lib.owt_fc_softmax_workspace_bytes(ctypes.byref(desc), pass_)
+    if n == ctypes.c_size_t(-1).value:
+        raise OwtError(OWT_EINVAL, owt_last_error())
+    return n
+
+
+def owt_fc_softmax_fwd(desc, x, w, bias, labels_or_null, lse, target_or_null=None, loss_or_null=None, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_lib.owt_fc_softmax_fwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(labels_or_null), _ptr(lse), _ptr(target_or_null),
+                                   _ptr(loss_or_null), p, n, _stream(stream)))
+
+
+def owt_softmax_join(workers, N, classes, lses, targets, labels, lse, target_or_null=None, loss_or_null=None, stream=None):
+    _check(_lib.owt_softmax_join(workers, N, classes, _ptr(lses), _ptr(targets), _ptr(labels), _ptr(lse), _ptr(target_or_null),
+                                 _ptr(loss_or_null), _stream(stream)))
+
+
+def owt_fc_softmax_bwd(desc, x, w, bias, labels, lse, weight_or_null, alpha, beta, dx_partial_or_null, dw, dbias_or_null, ws=None, stream=None):
+    p, n = _ws(ws)
+    _check(_lib.owt_fc_softmax_bwd(ctypes.byref(desc), _ptr(x), _ptr(w), _ptr(bias), _ptr(labels), _ptr(lse), _ptr(weight_or_null), alpha, beta,
+                                   _ptr(dx_partial_or_null), _ptr(dw), _ptr(dbias_or_null), p, n, _stream(stream)))
+
+
+class tensor_list:
+    """Tensors for the calls that take many: their pointers and sizes in the arrays that those calls read.  Made once, it keeps the tensors."""
+
+    def __init__(self, tensors):
+        self.tensors = tuple(tensors)
+        self.count = len(self.tensors)
+        self.sizes = tuple(t.numel() for t in self.tensors)
+        self.width = self.tensors[0].element_size() if self.count else 0
+        if any(t.element_size() != self.width for t in self.tensors):
+            raise ValueError("the tensors of a list are of one type")
+        self.at = (ctypes.c_void_p * max(1, self.count))(*[_ptr(t) for t in self.tensors])
+        self.n = (ctypes.c_size_t * max(1, self.count))(*self.sizes)
+
+    def like(self, other, width):
+        """Whether this list has tensors of other's sizes, of values of `width` bytes."""
+        return self.sizes == other.sizes and (self.width == width or not self.count)
+
+
+def _lists(dtype, first, *others):
+    width = 2 if dtype == OWT_BF16 else 4
+    if not all(l.like(first, w) for l, w in ((first, width),) + tuple((l, width) if not isinstance(l, tuple) else l for l in others)):
+        raise ValueError("lists of different sizes or types")
+
+
+def owt_grad_norm_workspace_bytes(g):
+    n = _lib.owt_grad_norm_workspace_bytes(g.count, g.n)
+    if n == ctypes.c_size_t(-1).value:
+        raise OwtError(OWT_EINVAL, owt_last_error())
+    return n
+
+
+def owt_grad_norm(g, dtype, norm, ws=None, stream=None):
+    _lists(dtype, g)
+    p, n = _ws(ws)
+    _check(_lib.owt_grad_norm(g.count, g.n, g.at, dtype, _ptr(norm), p, n, _stream(stream)))
+
+
+def owt_grad_clip(g, out, dtype, norm, max_norm, stream=None):
+    _lists(dtype, g, out)
+    _check(_lib.owt_grad_clip(g.count, g.n, g.at, out.at, dtype, _ptr(norm), max_norm, _stream(stream)))
+
+
+def owt_sgd_momentum_clipped(w, vel, g, mu, eps, omega, gscale, norm, max_norm, w_bf16=None, stream=None):
+    _lists(OWT_F32, w, vel, g, *([(w_bf16, 2)] if w_bf16 is not None else []))
+    _check(_lib.owt_sgd_momentum_clipped(w.count, w.n, w.at, vel.at, g.at, mu, eps, omega, gscale, _ptr(norm), max_norm,
+                                         None if w_bf16 is None else w_bf16.at, _stream(stream)))

@@ -1,0 +1,347 @@
+// The norm of the gradients of many tensors together, and what is done with it: the gradients times the factor that brings the norm down to a
+// bound, or the momentum / weight-decay update of Section 5 with the bounded gradients.  All three are HBM-bound passes over lists of tensors.
+//
+// A list is cut into chunks of 16 KB that end with their tensor; a work-group walks a run of consecutive chunks, 16 bytes an access.  Pointers
+// and sizes of up to kSet tensors travel in a launch's arguments (so that a captured launch holds them, and nothing is allocated); longer lists
+// take several launches.
+#include <cmath>
+
+#include "owt_host.hpp"
+
+namespace owt {
+
+constexpr int kClipGroups = 2048;       // eight work-groups of 256 threads a CU: all that run at a time
+constexpr int kSet = 80;                // tensors of a launch: with four pointers each 3.6 KB of arguments
+constexpr int kChunkBytes = 16384;      // of gradients: 64 bytes a thread
+
+// P pointers for each tensor; chunks [first[t], first[t + 1]) are tensor t's, and its last one has last[t] values.  Work-group b has each + (b < more)
+// chunks.  (All in 32 bits: compared in 64, the size that is left was taken for a whole chunk by the compiler's choice between the two.)
+template <int P> struct TensorSet {
+    void *at[P][kSet];
+    unsigned first[kSet + 1], last[kSet];
+    int count;
+    unsigned each, more;
+};
+
+// f(t, from, values) for each chunk of this work-group's run, `chunk` values at most
+template <int P, class F> __device__ __forceinline__ void walk_chunks(const TensorSet<P> &s, unsigned chunk, F f)
+{
+    const unsigned b = blockIdx.x;
+    unsigned c = b * s.each + min(b, s.more);
+    const unsigned end = c + s.each + (b < s.more ? 1 : 0);
+    int t = 0;
+    for (; c < end; c++) {
+        while (c >= s.first[t + 1]) t++;
+        const unsigned n = c + 1 == s.first[t + 1] ? s.last[t] : chunk;
+        f(t, (size_t)(c - s.first[t]) * chunk, n);
+    }
+}
+
+template <class T> constexpr int kPer = 16 / sizeof(T);             // values of an access
+template <class T> __device__ __forceinline__ void widen(const uint4 &v, float (&f)[kPer<T>])
+{
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+        if (sizeof(T) == 4) f[k] = __uint_as_float(u[k]);
+        else {
+            f[2 * k % kPer<T>] = __uint_as_float(u[k] << 16);
+            f[(2 * k + 1) % kPer<T>] = __uint_as_float(u[k] & 0xffff0000u);
+        }
+    }
+}
+template <class T> __device__ __forceinline__ uint4 narrow(const float (&f)[kPer<T>])
+{
+    uint32_t u[4];
+#pragma unroll
+    for (int k = 0; k < 4; k++)
+        u[k] = sizeof(T) == 4 ? __float_as_uint(f[k]) : f32x2_to_bf16x2(f[2 * k % kPer<T>], f[(2 * k + 1) % kPer<T>]);
+    return make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// A work-group's sum in a fixed order: lanes in pairs, then wavefronts one by one.  The result is thread 0's.
+template <int WAVES> __device__ __forceinline__ double group_sum(double v)
+{
+    __shared__ double part[WAVES];
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.;
+    if (threadIdx.x == 0)
+        for (int w = 0; w < WAVES; w++) v += part[w];
+    return v;
+}
+
+// Squares are summed in 64 bits: no gradient that fp32 holds overflows or vanishes in them, and the sum is as exact as its result's 32 bits
+// whatever the number of values.  (An instruction of 64 bits a value is half the fp32 rate, twenty times what memory brings.)
+template <class T, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) grad_square_kernel(const TensorSet<1> s, double *partial, float *norm)
+{
+    constexpr int V = kPer<T>, CH = kChunkBytes / sizeof(T), U = CH / (V * 64 * WAVES);
+    double sum[4] = {0., 0., 0., 0.};
+    auto add = [&](const uint4 &v) __attribute__((always_inline)) {
+        float f[V];
+        widen<T>(v, f);
+#pragma unroll
+        for (int k = 0; k < V; k++) sum[k & 3] = fma((double)f[k], (double)f[k], sum[k & 3]);
+    };
+    walk_chunks(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
+        const T *g = (const T *)s.at[0][t] + from;
+        if (n == CH) {
+            uint4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) v[u] = ((const uint4 *)g)[threadIdx.x + 64 * WAVES * u];
+#pragma unroll
+            for (int u = 0; u < U; u++) add(v[u]);
+        } else {
+            for (unsigned i = threadIdx.x; i < n / V; i += 64 * WAVES) add(((const uint4 *)g)[i]);
+            const unsigned i = n / V * V + threadIdx.x;
+            if (i < n) {
+                const double x = load1(g, (int)i);
+                sum[0] = fma(x, x, sum[0]);
+            }
+        }
+    });
+    const double all = group_sum<WAVES>((sum[0] + sum[1]) + (sum[2] + sum[3]));
+    if (threadIdx.x == 0) {
+        if (norm) *norm = (float)sqrt(all);         // the only work-group of the only launch
+        else partial[blockIdx.x] = all;
+    }
+}
+
+__global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *partial, int n, float *norm)
+{
+    double v = 0.;
+    for (int i = threadIdx.x; i < n; i += 1024) v += partial[i];
+    v = group_sum<16>(v);
+    if (threadIdx.x == 0) *norm = (float)sqrt(v);
+}
+
+// out = g * min(1, max / norm); zeros where the norm is not finite.  Gradients that stay as they are and where they are are not touched.
+template <class T>
+__global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, const float *norm, float max_norm)
+{
+    constexpr int V = kPer<T>, CH = kChunkBytes / sizeof(T), U = CH / (V * 256);
+    const float all = *norm;
+    const bool fine = __builtin_isfinite(all);
+    const float factor = fine ? fminf(1.f, max_norm / all) : 0.f;
+    auto scaled = [&](const uint4 &v) __attribute__((always_inline)) {
+        float f[V];
+        widen<T>(v, f);
+#pragma unroll
+        for (int k = 0; k < V; k++) f[k] = fine ? f[k] * factor : 0.f;
+        return narrow<T>(f);
+    };
+    walk_chunks(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
+        const T *g = (const T *)s.at[0][t] + from;
+        T *out = (T *)s.at[1][t] + from;
+        if (factor == 1.f && g == out) return;
+        if (n == CH) {
+            uint4 v[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) v[u] = ((const uint4 *)g)[threadIdx.x + 256 * u];
+#pragma unroll
+            for (int u = 0; u < U; u++) ((uint4 *)out)[threadIdx.x + 256 * u] = scaled(v[u]);
+        } else {
+            for (unsigned i = threadIdx.x; i < n / V; i += 256) ((uint4 *)out)[i] = scaled(((const uint4 *)g)[i]);
+            const unsigned i = n / V * V + threadIdx.x;
+            if (i < n) store1(out, i, fine ? load1(g, (int)i) * factor : 0.f);
+        }
+    });
+}
+
+// vel := mu*vel + eps*(gscale*factor*g - omega*w);  w := w + vel;  factor = min(1, max / (|gscale| norm)).  A norm that is not finite: no step.
+template <bool COPY>
+__global__ void __launch_bounds__(256) sgd_clipped_kernel(const TensorSet<3 + COPY> s, float mu, float eps, float omega, float gscale,
+                                                          const float *norm, float max_norm)
+{
+    constexpr int CH = kChunkBytes / 4, U = CH / 1024;
+    const float all = *norm;
+    if (!__builtin_isfinite(all)) return;
+    const double bounded = (double)max_norm / ((double)fabsf(gscale) * (double)all);        // (0 / 0 is no bound, either)
+    const float scale = bounded < 1. ? (float)(gscale * bounded) : gscale;
+    auto upd = [&](float &wv, float &vv, float gv) __attribute__((always_inline)) {
+        vv = fmaf(mu, vv, eps * fmaf(scale, gv, -omega * wv));
+        wv += vv;
+    };
+    walk_chunks(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
+        float *w = (float *)s.at[0][t] + from, *vel = (float *)s.at[1][t] + from;
+        const float *g = (const float *)s.at[2][t] + from;
+        uint16_t *wb = COPY ? (uint16_t *)s.at[2 + COPY][t] + from : nullptr;
+        auto put = [&](unsigned i, float4 a, float4 v, const float4 &d) __attribute__((always_inline)) {
+            upd(a.x, v.x, d.x); upd(a.y, v.y, d.y); upd(a.z, v.z, d.z); upd(a.w, v.w, d.w);
+            ((float4 *)vel)[i] = v;
+            ((float4 *)w)[i] = a;
+            if (COPY) ((uint2 *)wb)[i] = make_uint2(f32x2_to_bf16x2(a.x, a.y), f32x2_to_bf16x2(a.z, a.w));
+        };
+        if (n == CH) {
+            float4 a[U], v[U], d[U];
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                a[u] = ((const float4 *)w)[threadIdx.x + 256 * u];
+                v[u] = ((const float4 *)vel)[threadIdx.x + 256 * u];
+                d[u] = ((const float4 *)g)[threadIdx.x + 256 * u];
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) put(threadIdx.x + 256 * u, a[u], v[u], d[u]);
+        } else {
+            for (unsigned i = threadIdx.x; i < n / 4; i += 256) put(i, ((const float4 *)w)[i], ((const float4 *)vel)[i], ((const float4 *)g)[i]);
+            const unsigned i = n / 4 * 4 + threadIdx.x;
+            if (i < n) {
+                float a = w[i], v = vel[i];
+                upd(a, v, g[i]);
+                vel[i] = v; w[i] = a;
+                if (COPY) wb[i] = f32_to_bf16(a);
+            }
+        }
+    });
+}
+
+// ------------------------------------------------------------------------------------------------ host
+
+static size_t chunks_of(size_t n, size_t chunk) { return n / chunk + (n % chunk != 0); }
+
+// Sizes that a walk counts in 32 bits
+static owt_status check_list(int count, const size_t *n, size_t &chunks, size_t chunk)
+{
+    if (count < 0) return fail(OWT_EINVAL, "count must not be negative");
+    if (count > 0 && !n) return fail(OWT_EINVAL, "n is NULL");
+    chunks = 0;
+    for (int t = 0; t < count; t++) {
+        if (n[t] > ((size_t)1 << 40)) return fail(OWT_EUNSUPPORTED, "tensor %d has more than 2^40 values", t);
+        chunks += chunks_of(n[t], chunk);
+        if (chunks > 0x7fffffffu) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 chunks of 16 KB");
+    }
+    return OWT_OK;
+}
+static owt_status check_pointers(int count, const size_t *n, const void *const *p, const char *what)
+{
+    if (count > 0 && !p) return fail(OWT_EINVAL, "%s is NULL", what);
+    for (int t = 0; t < count; t++)
+        if (n[t]) {
+            if (!p[t]) return fail(OWT_EINVAL, "%s[%d] is NULL", what, t);
+            if (!aligned16(p[t])) return fail(OWT_EINVAL, "%s[%d] is not 16-byte aligned", what, t);
+        }
+    return OWT_OK;
+}
+static int values_of_chunk(owt_dtype dtype) { return kChunkBytes / (dtype == OWT_BF16 ? 2 : 4); }
+
+// go(set, work-groups) for each kSet tensors that are not empty
+template <int P, class F> static owt_status for_sets(int count, const size_t *n, const void *const *const (&at)[P], size_t chunk, F go)
+{
+    TensorSet<P> s;
+    s.count = 0;
+    s.first[0] = 0;
+    for (int t = 0; t <= count; t++) {
+        if (s.count == kSet || (t == count && s.count > 0)) {
+            const unsigned chunks = s.first[s.count], groups = chunks < (unsigned)kClipGroups ? chunks : (unsigned)kClipGroups;
+            s.each = chunks / groups;
+            s.more = chunks % groups;
+            go(s, groups);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess) return fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+            s.count = 0;
+        }
+        if (t == count || n[t] == 0) continue;
+        for (int k = 0; k < P; k++) s.at[k][s.count] = const_cast<void *>(at[k][t]);
+        s.last[s.count] = (unsigned)((n[t] - 1) % chunk) + 1;
+        s.first[s.count + 1] = s.first[s.count] + (unsigned)chunks_of(n[t], chunk);
+        s.count++;
+    }
+    return OWT_OK;
+}
+static size_t sets_of(int count, const size_t *n)
+{
+    size_t full = 0;
+    for (int t = 0; t < count; t++) full += n[t] != 0;
+    return (full + kSet - 1) / kSet;
+}
+
+}  // namespace owt
+
+using namespace owt;
+#define OWT_TRY(e) do { const owt_status st_ = (e); if (st_ != OWT_OK) return st_; } while (0)
+
+extern "C" {
+
+size_t owt_grad_norm_workspace_bytes(int count, const size_t *n)
+{
+    size_t chunks;
+    if (check_list(count, n, chunks, values_of_chunk(OWT_F32)) != OWT_OK) return (size_t)-1;
+    return sets_of(count, n) * kClipGroups * sizeof(double);
+}
+
+owt_status owt_grad_norm(int count, const size_t *n, const void *const *g, owt_dtype dtype, float *norm, void *ws, size_t ws_bytes, void *hip_stream)
+{
+    if (dtype != OWT_F32 && dtype != OWT_BF16) return fail(OWT_EINVAL, "unknown dtype %d", (int)dtype);
+    const int chunk = values_of_chunk(dtype);
+    size_t chunks;
+    OWT_TRY(check_list(count, n, chunks, chunk));
+    OWT_TRY(check_pointers(count, n, g, "g"));
+    if (!norm || !aligned16(norm)) return fail(OWT_EINVAL, "norm is NULL or not 16-byte aligned");
+    const size_t sets = sets_of(count, n), need = sets * kClipGroups * sizeof(double);
+    if (ws_bytes < need) return fail(OWT_EWORKSPACE, "workspace too small: need %zu bytes, got %zu", need, ws_bytes);
+    if (need && (!ws || !aligned16(ws))) return fail(OWT_EINVAL, "ws is NULL or misaligned");
+    hipStream_t s = (hipStream_t)hip_stream;
+    double *partial = (double *)ws;
+    int parts = 0;
+    OWT_TRY(for_sets<1>(count, n, {g}, chunk, [&](const TensorSet<1> &set, unsigned groups) {
+        if (dtype == OWT_F32) hipLaunchKernelGGL((grad_square_kernel<float, 4>), dim3(groups), dim3(256), 0, s, set, partial + parts, (float *)nullptr);
+        else hipLaunchKernelGGL((grad_square_kernel<bf16_t, 4>), dim3(groups), dim3(256), 0, s, set, partial + parts, (float *)nullptr);
+        parts += (int)groups;
+    }));
+    hipLaunchKernelGGL(grad_norm_join_kernel, dim3(1), dim3(1024), 0, s, partial, parts, norm);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+}
+
+static owt_status check_bound(const float *norm, float max_norm)
+{
+    if (!norm || !aligned16(norm)) return fail(OWT_EINVAL, "norm is NULL or not 16-byte aligned");
+    if (!(max_norm > 0.f)) return fail(OWT_EINVAL, "max_norm must be positive");
+    return OWT_OK;
+}
+
+owt_status owt_grad_clip(int count, const size_t *n, const void *const *g, void *const *out, owt_dtype dtype, const float *norm, float max_norm,
+                         void *hip_stream)
+{
+    if (dtype != OWT_F32 && dtype != OWT_BF16) return fail(OWT_EINVAL, "unknown dtype %d", (int)dtype);
+    const int chunk = values_of_chunk(dtype);
+    size_t chunks;
+    OWT_TRY(check_list(count, n, chunks, chunk));
+    OWT_TRY(check_pointers(count, n, g, "g"));
+    OWT_TRY(check_pointers(count, n, out, "out"));
+    OWT_TRY(check_bound(norm, max_norm));
+    hipStream_t s = (hipStream_t)hip_stream;
+    return for_sets<2>(count, n, {g, out}, chunk, [&](const TensorSet<2> &set, unsigned groups) {
+        if (dtype == OWT_F32) hipLaunchKernelGGL(grad_clip_kernel<float>, dim3(groups), dim3(256), 0, s, set, norm, max_norm);
+        else hipLaunchKernelGGL(grad_clip_kernel<bf16_t>, dim3(groups), dim3(256), 0, s, set, norm, max_norm);
+    });
+}
+
+owt_status owt_sgd_momentum_clipped(int count, const size_t *n, float *const *w, float *const *vel, const float *const *g, float mu, float eps,
+                                    float omega, float gscale, const float *norm, float max_norm, void *const *w_bf16_or_null, void *hip_stream)
+{
+    const int chunk = values_of_chunk(OWT_F32);
+    size_t chunks;
+    OWT_TRY(check_list(count, n, chunks, chunk));
+    OWT_TRY(check_pointers(count, n, (const void *const *)w, "w"));
+    OWT_TRY(check_pointers(count, n, (const void *const *)vel, "vel"));
+    OWT_TRY(check_pointers(count, n, (const void *const *)g, "g"));
+    if (w_bf16_or_null) OWT_TRY(check_pointers(count, n, w_bf16_or_null, "w_bf16"));
+    if (!std::isfinite(mu) || !std::isfinite(eps) || !std::isfinite(omega) || !std::isfinite(gscale))
+        return fail(OWT_EINVAL, "mu, eps, omega and gscale must be finite");
+    OWT_TRY(check_bound(norm, max_norm));
+    hipStream_t s = (hipStream_t)hip_stream;
+    const void *const *W = (const void *const *)w, *const *V = (const void *const *)vel, *const *G = (const void *const *)g;
+    if (w_bf16_or_null)
+        return for_sets<4>(count, n, {W, V, G, w_bf16_or_null}, chunk, [&](const TensorSet<4> &set, unsigned groups) {
+            hipLaunchKernelGGL(sgd_clipped_kernel<true>, dim3(groups), dim3(256), 0, s, set, mu, eps, omega, gscale, norm, max_norm);
+        });
+    return for_sets<3>(count, n, {W, V, G}, chunk, [&](const TensorSet<3> &set, unsigned groups) {
+        hipLaunchKernelGGL(sgd_clipped_kernel<false>, dim3(groups), dim3(256), 0, s, set, mu, eps, omega, gscale, norm, max_norm);
+    });
+}
+
+}  // extern "C"
