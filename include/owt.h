@@ -329,11 +329,13 @@ size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass);     /* (
  * OWT_BIAS (the only flag).  labels [N]: class index in the whole layer.  A row whose label is outside [0, O_total) has no class: it is padding,
  * whatever its x holds (infinities and NaN, too) has no influence on any other row, its lse, target, loss and dx are 0.
  * A bias of -infinity takes a class out: it adds nothing to lse and gets no gradient.  N == 0 is an empty batch.
- * N, O_local <= 2^22 and x and w of at most 2^31-1 values (OWT_EUNSUPPORTED).
+ * N, I, O_local <= 2^22, x and w of at most 2^31-1 values, no more tiles of outputs than a launch counts (OWT_EUNSUPPORTED).
  *
- * bf16 operands are multiplied as they are.  fp32 ones may be multiplied as sums of two f16 values under a power of two for each row of x and of w
- * (in the backward pass also of dz), which hold 22 bits of all that is within 2^-16 of the row's largest magnitude, and 2^-39 of the largest below that.
- * dz meets x, for dw, as the sum of two values of 8 (bf16) or 11 bits, and w, for dx, as one in bf16: dx is rounded to bf16 itself. */
+ * bf16 operands are multiplied as they are.  fp32 ones may be multiplied as sums of two f16 values under a power of two for each row of x and of w,
+ * which hold 22 bits of all that is within 2^-16 of the row's largest magnitude, and 2^-39 of the largest below that.  dz meets x, for dw, as the sum of
+ * two bf16 values (16 bits) or of two f16 ones, and w, for dx, as one bf16 value (dx is rounded to bf16 itself) or as two f16 ones.  f16 values of dz are under
+ * one power of two for all rows: of exp(z - lse) and of 1 they hold 22 bits down to 2^-18, and 2^-40 below that (where rows of x, with their weights, or
+ * of w differ in size, times the ratio of the largest row's largest magnitude to that of the row that is met, and up to four). */
 
 /* Forward pass:  lse[n] = log sum_o exp z[n][o] (-infinity where every output is);  target[n] = z[n][label] if the label is one of this worker's
  * columns, else -infinity;  loss[n] = lse[n] - target[n] (+infinity for a class that is taken out).  All [N] fp32.  labels may be NULL (then target and

@@ -41,6 +41,9 @@ def _units():
     for ps, pname in ((0, "fwd"), (1, "data")):
         units.append(("xconvs_%s.o" % pname, "xconvs_inst.hip", ["-DOWT_INST_PASS=%d" % ps]))
         units.append(("dconv16s_%s.o" % pname, "dconv16s_inst.hip", ["-DOWT_INST_PASS=%d" % ps]))
+    for half, hname in ((0, "bf16"), (1, "half")):
+        for out, oname in ((0, "ends"), (1, "out")):
+            units.append(("softmax_%s_%s.o" % (hname, oname), "softmax_inst.hip", ["-DOWT_INST_HALF=%d" % half, "-DOWT_INST_OUT=%d" % out]))
     units.append(("xfilter.o", "xfilter_inst.hip", []))
     units.append(("xgather.o", "xgather_inst.hip", []))
     for masked in (0, 1):

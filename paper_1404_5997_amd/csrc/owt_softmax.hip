@@ -1,143 +1,292 @@
-// Softmax cross-entropy on a dense shard's outputs, without the outputs: entry points, and kernels that are right for every size.
+// Softmax cross-entropy on a dense shard's outputs, without the outputs: entry points, and the passes around the products of smgemm.hpp.
 //
 //   z[n][o] = bias[o] + sum_i x[n][i] w[o][i],   lse[n] = log sum_o exp z[n][o]
 //   dz[n][o] = weight[n] (exp(z[n][o] - lse[n]) - [o is n's label]),   dx = dz w,   dw = alpha dz^T x + beta dw,   dbias likewise
 //
-// The classes are taken in pieces whose outputs fit the scratch; of a piece there is left the largest output and the sum of exponentials
-// below it for each row (forward), or its part of dx and its rows of dw (backward, which computes the outputs again).
+// Forward, a product's work-groups leave each row's largest output and sum of exponentials over their columns, and one launch joins those.  Backward,
+// the classes are taken in pieces: the outputs of a piece are computed again and leave as dz, its part of dx is added up and its rows of dw
+// are done.  Where a product has few tiles its sums are split over work-groups, and the launch that joins them does the same to the outputs.
+//
+// bf16 weights whose rows are whole steps of 64 values are read as they lie; others, and fp32 operands, are laid out for the products first, fp32
+// values as two f16 ones.
 #include <cmath>
 
-#include "owt_host.hpp"
+#include "softmax.hpp"
 
 namespace owt {
 
-constexpr int kPiece = 4096;            // classes of a piece
+// ------------------------------------------------------------------------------------------------ layout of operands
 
-struct SimpleProduct {
-    const void *a, *b;                  // A[m][k] at m am + k ak, B[c][k] at c bc + k bk
-    long am, ak, bc, bk;
-    const int *rows;                    // labels of the rows that k counts: B is zero where there is none (may be null)
+struct SmPrep {
+    const void *from;           // [rows][cols]
+    unsigned char *to;          // rows of `steps` steps
+    int rows, out_rows, cols, steps;
+    const int *labels;          // rows without a class become zeros (null: none do)
     int classes;
-    int M, N;
-    long K;
-    const float *bias;                  // of columns, or null
-    float alpha, beta;
-    void *out;
-    long ldo;
+    const float *weight;        // of the rows, or null
+    int *exps;                  // fp32: of each row
+    // fp32: [0] takes the least of x's exponents less those of the weights, [1 + piece] those of w's pieces.  Laying out x sets all of them; the first
+    // piece's w finds the first, from x's exponents (x_rows of them) by work-groups of its own.
+    int *least, leasts, piece;
+    const int *x_exps;
+    int x_rows;
 };
 
-__device__ __forceinline__ bool has_class(int label, int classes) { return (unsigned)label < (unsigned)classes; }
-
-// 64 x 64 results a work-group, 4 x 4 a thread, 16 of k a step
-template <class TA, class TB, class TO>
-__global__ void __launch_bounds__(256) simple_product_kernel(const SimpleProduct p)
+// bf16 rows to whole steps, zeros behind them
+__global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep p)
 {
-    __shared__ float as[16][65], bs[16][65];
-    const int tid = threadIdx.x, tm = tid / 16, tc = tid % 16;
-    const int m0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-    float acc[4][4] = {};
-    for (long k0 = 0; k0 < p.K; k0 += 16) {
-        for (int e = tid; e < 1024; e += 256) {
-            const bool across = p.ak != 1;
-            const int r = across ? e % 64 : e / 16, k = across ? e / 64 : e % 16;
-            const long kk = k0 + k;
-            as[k][r] = m0 + r < p.M && kk < p.K ? load1((const TA *)p.a + (m0 + r) * p.am + kk * p.ak, 0) : 0.f;
+    const size_t all = (size_t)p.out_rows * p.steps * 8, stride = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += stride) {
+        const int m = (int)(i / (unsigned)(p.steps * 8)), c = (int)(i % (unsigned)(p.steps * 8)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (m < p.rows && c < p.cols && (!p.labels || has_class(p.labels[m], p.classes))) {
+            const uint16_t *row = (const uint16_t *)p.from + (size_t)m * p.cols;
+            if ((p.cols & 7) == 0) v = *(const uint4 *)(row + c);
+            else {
+                uint32_t u[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const int a = c + 2 * k;
+                    u[k] = (a < p.cols ? row[a] : 0u) | ((a + 1 < p.cols ? (uint32_t)row[a + 1] : 0u) << 16);
+                }
+                v = make_uint4(u[0], u[1], u[2], u[3]);
+            }
         }
-        for (int e = tid; e < 1024; e += 256) {
-            const bool across = p.bk != 1;
-            const int r = across ? e % 64 : e / 16, k = across ? e / 64 : e % 16;
-            const long kk = k0 + k;
-            bs[k][r] = c0 + r < p.N && kk < p.K && (!p.rows || has_class(p.rows[kk], p.classes)) ? load1((const TB *)p.b + (c0 + r) * p.bc + kk * p.bk, 0) : 0.f;
+        *(uint4 *)(p.to + i * 16) = v;
+    }
+}
+
+__device__ __forceinline__ int least_of_wave(int v)
+{
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v = min(v, __shfl_xor(v, d, 64));
+    return v;
+}
+
+// fp32 rows as two f16 values under the power of two that brings a row's largest magnitude to [2^14, 2^15), one wavefront a row.  The row is read twice,
+// the second time from the caches.
+__global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = (p.out_rows + 3) / 4;
+    if ((int)blockIdx.x >= groups) {        // the least exponent of x's rows with their weights
+        int least = kSmNone;
+        for (int n = ((int)blockIdx.x - groups) * 256 + threadIdx.x; n < p.x_rows; n += ((int)gridDim.x - groups) * 256) {
+            const float g = p.weight ? fabsf(p.weight[n]) : 1.f;
+            // a weight is below 2^k (one that is zero or not finite says nothing)
+            if (p.x_exps[n] != kSmNone && g > 0.f && __builtin_isfinite(g)) least = min(least, p.x_exps[n] - (ilogbf(g) + 1));
         }
+        least = least_of_wave(least);
+        if (lane == 0) atomicMin(p.least, least);
+        return;
+    }
+    if (p.leasts && blockIdx.x == 0)        // x: before anything looks for them
+        for (int i = threadIdx.x; i < p.leasts; i += 256) p.least[i] = kSmNone;
+    const int m = blockIdx.x * 4 + wave;
+    int exp = kSmNone;
+    if (m < p.out_rows) {
+        const bool real = m < p.rows && (!p.labels || has_class(p.labels[m], p.classes));
+        const float *row = (const float *)p.from + (size_t)m * p.cols;
+        const bool vec = (p.cols & 3) == 0;
+        auto four = [&](int c) __attribute__((always_inline)) {
+            if (!real || c >= p.cols) return make_float4(0.f, 0.f, 0.f, 0.f);
+            if (vec) return *(const float4 *)(row + c);
+            return make_float4(row[c], c + 1 < p.cols ? row[c + 1] : 0.f, c + 2 < p.cols ? row[c + 2] : 0.f, c + 3 < p.cols ? row[c + 3] : 0.f);
+        };
+        float most = 0.f;
+        if (real)
+#pragma unroll 4
+            for (int c = 4 * lane; c < p.cols; c += 256) {
+                const float4 v = four(c);
+                most = fmaxf(fmaxf(fmaxf(most, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
+            }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+        // (a row of infinities stays as it is: they are infinite in f16, too)
+        if (most > 0.f) exp = __builtin_isfinite(most) ? kSmTop - ilogbf(most) : 0;
+        const int shift = exp == kSmNone ? 0 : exp;     // (NaN alone has no largest magnitude, and stays NaN)
+        unsigned char *to = p.to + (size_t)m * p.steps * 256;
+#pragma unroll 4
+        for (int c = 4 * lane; c < p.steps * 64; c += 256) {
+            const float4 v = four(c);
+            const float s[4] = {ldexpf(v.x, shift), ldexpf(v.y, shift), ldexpf(v.z, shift), ldexpf(v.w, shift)};
+            sm_put_halves(to + (size_t)(c >> 6) * 256 + 2 * (c & 63), s);
+        }
+        if (lane == 0 && m < p.rows) p.exps[m] = exp;
+    }
+    if (p.piece >= 0) {
+        __shared__ int part[4];
+        if (lane == 0) part[wave] = exp;
         __syncthreads();
-        for (int k = 0; k < 16; k++)
-#pragma unroll
-            for (int i = 0; i < 4; i++)
-#pragma unroll
-                for (int j = 0; j < 4; j++) acc[i][j] = fmaf(as[k][tm * 4 + i], bs[k][tc * 4 + j], acc[i][j]);
+        if (threadIdx.x == 0) atomicMin(p.least + 1 + p.piece, min(min(part[0], part[1]), min(part[2], part[3])));
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ after the products
+
+__device__ __forceinline__ float lse_of(Top t) { return (__builtin_isfinite(t.max) ? t.max : 0.f) + logf(t.sum); }
+__device__ __forceinline__ float loss_of(float lse, float target) { return target == -INFINITY ? INFINITY : lse - target; }
+
+struct SmRows {                 // what is known of rows of outputs, and where it goes
+    const Top *top;             // [parts][N]
+    int parts, N;
+    const float *label_out;     // outputs of the labels that these columns hold
+    const int *labels;
+    int classes, off, cols;     // this worker's columns
+    float *lse, *target, *loss;
+};
+__device__ __forceinline__ void finish_row(const SmRows &p, int n, Top t, const float *label_out)
+{
+    float lse = lse_of(t), target = -INFINITY, loss = 0.f;
+    if (p.labels) {
+        const int label = p.labels[n];
+        if (!has_class(label, p.classes)) lse = target = 0.f;
+        else {
+            if (label >= p.off && label - p.off < p.cols) target = *label_out;
+            loss = loss_of(lse, target);
+        }
+        if (p.target) p.target[n] = target;
+        if (p.loss) p.loss[n] = loss;
+    }
+    p.lse[n] = lse;
+}
+// Joins the parts of 256 / EACH rows in a work-group, EACH threads a row
+template <int EACH> __global__ void __launch_bounds__(256) sm_finish_kernel(const SmRows p)
+{
+    constexpr int ROWS = 256 / EACH;
+    __shared__ Top part[EACH][ROWS];
+    const int r = threadIdx.x % ROWS, e = threadIdx.x / ROWS, n = blockIdx.x * ROWS + r;
+    Top t = {-INFINITY, 0.f};
+    if (n < p.N)
+        for (int k = e; k < p.parts; k += EACH) t = join(t, p.top[(size_t)k * p.N + n]);
+    part[e][r] = t;
+    __syncthreads();
+    for (int half = EACH / 2; half >= 1; half /= 2) {
+        if (e < half) part[e][r] = join(part[e][r], part[e + half][r]);
         __syncthreads();
     }
-    for (int i = 0; i < 4; i++)
-        for (int j = 0; j < 4; j++) {
-            const int m = m0 + tm * 4 + i, c = c0 + tc * 4 + j;
-            if (m >= p.M || c >= p.N) continue;
-            float v = p.alpha * acc[i][j];
-            if (p.bias) v += p.bias[c];
-            TO *to = (TO *)p.out + m * p.ldo + c;
-            if (p.beta != 0.f) v += p.beta * load1(to, 0);
-            store1(to, 0, v);
-        }
+    if (e == 0 && n < p.N) finish_row(p, n, part[0][r], p.label_out + n);
 }
 
-// The largest output of a row and the sum of exponentials below it, joined with another such pair.  A pair without outputs is (-inf, 0); outputs
-// of -inf add nothing; +inf and NaN leave as infinity and NaN.
-struct Top { float max, sum; };
-__device__ __forceinline__ Top top_of(float v) { return {v == v ? v : 0.f, v == -INFINITY ? 0.f : v == INFINITY || v != v ? v : 1.f}; }
-__device__ __forceinline__ Top join(Top a, Top b)
+// Outputs whose sums were split: a work-group a row joins them and is done with it.
+template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_top_kernel(const SmParams p, const SmRows r)
 {
-    const float m = fmaxf(a.max, b.max), at = __builtin_isfinite(m) ? m : 0.f;
-    return {m, a.sum * (a.max == m ? 1.f : expf(a.max - at)) + b.sum * (b.max == m ? 1.f : expf(b.max - at))};
-}
-
-// One wavefront a row: row n's pair over these columns, joined with what pieces before left, and the label's output.
-__global__ void __launch_bounds__(256) piece_top_kernel(const float *z, int N, int cols, int off, const int *labels, int classes, bool first, Top *top,
-                                                        float *target)
-{
-    const int n = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
-    if (n >= N) return;
+    __shared__ Top part[4];
+    __shared__ float label_out;
+    const int m = blockIdx.x, at = p.labels ? p.labels[m] - p.off : -1;
+    const size_t whole = (size_t)p.M * p.N;
+    const float *row = p.partial + (size_t)m * p.N;
+    const int re = SCALED ? p.row_exp[m] : 0;
     Top t = {-INFINITY, 0.f};
-    for (int j = lane; j < cols; j += 64) {
-        t = join(t, top_of(z[(size_t)n * cols + j]));
+    for (int c = threadIdx.x; c < p.N; c += 256) {
+        float z = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < p.splits; k++) z += row[k * whole + c];
+        if (SCALED) z = ldexpf(z, -(re + p.col_exp[c]));
+        if (p.bias) z += p.bias[c];
+        if (c == at) label_out = z;
+        t = join(t, top_of(z));
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) t = join(t, {__shfl_xor(t.max, d, 64), __shfl_xor(t.sum, d, 64)});
-    if (lane == 0) {
-        top[n] = first ? t : join(top[n], t);
-        const int j = labels ? labels[n] - off : -1;
-        if (target) {
-            if (first) target[n] = -INFINITY;
-            if (labels && has_class(labels[n], classes) && j >= 0 && j < cols) target[n] = z[(size_t)n * cols + j];
-        }
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = t;
+    __syncthreads();
+    if (threadIdx.x == 0) finish_row(r, m, join(join(part[0], part[1]), join(part[2], part[3])), &label_out);
+}
+
+// dz of outputs whose sums were split: 32 rows by 64 columns a work-group, 16 threads a row
+template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_dz_kernel(const SmParams p)
+{
+    __shared__ float4 part[16][16];
+    const int q = threadIdx.x & 15, r = threadIdx.x >> 4, c = blockIdx.x * 64 + 4 * q;
+    const size_t whole = (size_t)p.M * p.N;
+    const SmDzColumns k = sm_dz_columns<SCALED>(p, c);
+    float sums[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int m = blockIdx.y * 32 + r; m < min(p.M, (int)blockIdx.y * 32 + 32); m += 16) {
+        float z[4] = {0.f, 0.f, 0.f, 0.f};
+        const float *row = p.partial + (size_t)m * p.N + c;
+        if ((p.N & 3) == 0) {
+            if (c < p.N)
+#pragma unroll 4
+                for (int s = 0; s < p.splits; s++) {
+                    const float4 v = *(const float4 *)(row + s * whole);
+                    z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w;
+                }
+        } else
+            for (int s = 0; s < p.splits; s++)
+#pragma unroll
+                for (int t = 0; t < 4; t++)
+                    if (c + t < p.N) z[t] += row[s * whole + t];
+        sm_dz<SCALED>(p, m, c, make_float4(z[0], z[1], z[2], z[3]), sm_dz_row<SCALED>(p, m), k, sums);
+    }
+    if (!p.dbias) return;
+    part[r][q] = make_float4(sums[0], sums[1], sums[2], sums[3]);
+    __syncthreads();
+    if (threadIdx.x < 64 && blockIdx.x * 64 + threadIdx.x < p.N) {
+        float s = 0.f;
+        for (int k2 = 0; k2 < 16; k2++) s += ((const float *)&part[k2][threadIdx.x >> 2])[threadIdx.x & 3];
+        p.dbias[(size_t)blockIdx.y * p.N + blockIdx.x * 64 + threadIdx.x] = s;
     }
 }
 
-__device__ __forceinline__ float loss_of(float lse, float target) { return target == -INFINITY ? INFINITY : lse - target; }
-
-__global__ void __launch_bounds__(256) lse_kernel(int N, const Top *top, const int *labels, int classes, float *lse, float *target, float *loss)
+// Adds up the parts of a split sum, in order: four columns a thread.  No parts: a sum of nothing.
+template <bool SCALED> __global__ void __launch_bounds__(256) sm_join_kernel(const SmParams p)
 {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
-    const Top t = top[n];
-    float l = (__builtin_isfinite(t.max) ? t.max : 0.f) + logf(t.sum);
-    if (labels && !has_class(labels[n], classes)) {
-        l = 0.f;
-        if (target) target[n] = 0.f;
-        if (loss) loss[n] = 0.f;
-    } else if (loss) loss[n] = loss_of(l, target[n]);
-    lse[n] = l;
+    const unsigned quads = (unsigned)(p.N + 3) / 4;
+    const size_t n = (size_t)p.M * quads, stride = (size_t)gridDim.x * 256, whole = (size_t)p.M * p.N;
+    const int shift = SCALED && p.splits ? -(*p.least + kSmDzTop) : 0;
+    const bool vec = (p.N & 3) == 0;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
+        const int m = (int)(i / quads), c = (int)(i % quads) * 4;
+        const size_t at = (size_t)m * p.N + c;
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        auto four = [&](const float *from, float (&u)[4]) __attribute__((always_inline)) {
+            if (vec) {
+                const float4 w = *(const float4 *)from;
+                u[0] = w.x; u[1] = w.y; u[2] = w.z; u[3] = w.w;
+            } else
+#pragma unroll
+                for (int t = 0; t < 4; t++) u[t] = c + t < p.N ? from[t] : 0.f;
+        };
+#pragma unroll 4
+        for (int k = 0; k < p.splits; k++) {
+            float u[4];
+            four(p.partial + k * whole + at, u);
+#pragma unroll
+            for (int t = 0; t < 4; t++) v[t] += u[t];
+        }
+        sm_result<SCALED>(v, shift, sm_row_factor<SCALED>(p, m), p.alpha);
+        float u[4];
+        if (p.add) {
+            four(p.add + at, u);
+#pragma unroll
+            for (int t = 0; t < 4; t++) v[t] += u[t];
+        }
+        if (!p.bf16 && p.beta != 0.f) {
+            four((const float *)p.out + at, u);
+#pragma unroll
+            for (int t = 0; t < 4; t++) v[t] += p.beta * u[t];
+        }
+        if (vec && !p.bf16) *(float4 *)((float *)p.out + at) = make_float4(v[0], v[1], v[2], v[3]);
+        else if (vec) *(uint2 *)((uint16_t *)p.out + at) = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
+        else
+#pragma unroll
+            for (int t = 0; t < 4; t++)
+                if (c + t < p.N) {
+                    if (p.bf16) store1((bf16_t *)p.out, at + t, v[t]);
+                    else store1((float *)p.out, at + t, v[t]);
+                }
+    }
 }
 
-// outputs to their gradients, in place
-__global__ void __launch_bounds__(256) piece_dz_kernel(float *z, int N, int cols, int off, const int *labels, int classes, const float *lse, const float *weight)
+// dbias from the sums over strips of rows
+__global__ void __launch_bounds__(256) sm_dbias_kernel(const float *sums, int strips, int cols, float alpha, float beta, float *db)
 {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= (size_t)N * cols) return;
-    const int n = (int)(i / cols), j = (int)(i % cols), label = labels[n];
-    const float l = lse[n], v = z[i], p = v == -INFINITY ? 0.f : expf(v - l);
-    z[i] = has_class(label, classes) ? (weight ? weight[n] : 1.f) * (p - (j == label - off ? 1.f : 0.f)) : 0.f;
-}
-__global__ void __launch_bounds__(256) piece_dbias_kernel(const float *dz, int N, int cols, float alpha, float beta, float *db)
-{
-    const int j = blockIdx.x * 256 + threadIdx.x;
-    if (j >= cols) return;
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= cols) return;
     float s = 0.f;
-    for (int n = 0; n < N; n++) s += dz[(size_t)n * cols + j];
-    db[j] = alpha * s + (beta != 0.f ? beta * db[j] : 0.f);
-}
-template <class T> __global__ void __launch_bounds__(256) store_rows_kernel(const float *from, size_t n, int cols, const int *labels, int classes, T *to)
-{
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) store1(to, i, has_class(labels[i / cols], classes) ? from[i] : 0.f);
+#pragma unroll 8
+    for (int k = 0; k < strips; k++) s += sums[(size_t)k * cols + c];
+    db[c] = alpha * s + (beta != 0.f ? beta * db[c] : 0.f);
 }
 
 // Joins the shards' shares: lse and target of `workers` shards, worker by worker.
@@ -158,7 +307,7 @@ __global__ void __launch_bounds__(256) softmax_join_kernel(int workers, int N, i
         t = join(t, top_of(lses[(size_t)k * N + n]));
         at = __builtin_elementwise_maximum(at, targets[(size_t)k * N + n]);
     }
-    const float l = (__builtin_isfinite(t.max) ? t.max : 0.f) + logf(t.sum);
+    const float l = lse_of(t);
     lse[n] = l;
     if (target) target[n] = at;
     if (loss) loss[n] = loss_of(l, at);
@@ -166,7 +315,7 @@ __global__ void __launch_bounds__(256) softmax_join_kernel(int workers, int N, i
 
 // ------------------------------------------------------------------------------------------------ host
 
-constexpr int kMaxRows = 1 << 22;       // of x and of w
+constexpr int kMaxRows = 1 << 22;       // of x and of w, and values of a row: 256 rows of 2^24 bytes are addressed with 32 bits
 
 static owt_status check_softmax(const owt_fc_desc *d, int &o_local)
 {
@@ -178,7 +327,7 @@ static owt_status check_softmax(const owt_fc_desc *d, int &o_local)
     if (d->dtype != OWT_F32 && d->dtype != OWT_BF16) return fail(OWT_EINVAL, "unknown dtype %d", (int)d->dtype);
     if (d->flags & ~(unsigned)OWT_BIAS) return fail(OWT_EINVAL, "flags other than OWT_BIAS (0x%x) have no meaning here", d->flags);
     o_local = d->O_total / d->workers;
-    if (d->N > kMaxRows || o_local > kMaxRows) return fail(OWT_EUNSUPPORTED, "more than 2^22 rows or columns");
+    if (d->N > kMaxRows || o_local > kMaxRows || d->I > kMaxRows) return fail(OWT_EUNSUPPORTED, "more than 2^22 rows, columns or inputs");
     if ((long)d->N * d->I > 0x7fffffffL || (long)o_local * d->I > 0x7fffffffL) return fail(OWT_EUNSUPPORTED, "more than 2^31-1 elements");
     return OWT_OK;
 }
@@ -194,76 +343,343 @@ static owt_status need_ws(const void *ws, size_t have, size_t need)
     if (need && (!ws || !aligned16(ws))) return fail(OWT_EINVAL, "ws is NULL or misaligned");
     return OWT_OK;
 }
-static owt_status launched()
-{
-    const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
-}
 
-struct SoftmaxLayout {
-    size_t z, top, dx, total;
-    SoftmaxLayout(const owt_fc_desc *d, int ol, bool forward)
+// What a work-group takes: `start` for its beginning and end, `step` for a step on a quiet chip, `busy` where 128 or more run (256 x 256: all 256).
+struct SmTileCost { int bm, bn, wm, wn; float start, step, busy; };
+static const SmTileCost kSmTiles[SM_TILES] = {{256, 256, 2, 2, 11.f, 1.05f, 1.5f}, {128, 128, 2, 2, 3.f, 0.4f, 0.55f}, {64, 64, 2, 2, 1.2f, 0.21f, 0.21f},
+                                              {32, 256, 1, 4, 2.f, 0.3f, 1.0f}};
+constexpr int SM_NOTHING = -1;          // more work-groups than a launch holds
+struct SmPlan { int tile, splits; float us; };
+static int up(int n, int to) { return (n + to - 1) / to; }
+
+// `outputs`: sums that are split cost a pass over N x cols of them; results of dx and dw do, too
+static SmPlan sm_plan(long M, long N, int steps, bool few)
+{
+    SmPlan best{SM_NOTHING, 1, 1e30f};
+    const int want = forced_tile() - kSmFirstTile, want_split = forced_split();
+    for (int t = 0; t < SM_TILES; t++) {
+        if (t == SM_FEW && !few) continue;
+        if (want >= 0 && want < SM_TILES && t != want && (want != SM_FEW || few)) continue;
+        const SmTileCost &q = kSmTiles[t];
+        const long tiles = ((M + q.bm - 1) / q.bm) * ((N + q.bn - 1) / q.bn);
+        if (!groups_fit(tiles, 256)) continue;
+        for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= steps && tiles * sp <= 1024)); sp *= 2) {
+            const long each = (tiles * sp + 255) / 256;         // work-groups of a CU
+            const float step = tiles * sp >= (t == SM_BIG ? 256 : 128) ? q.busy : q.step;
+            float us = 3.f + (float)each * (q.start + (float)up(steps, sp) * step);
+            if (sp > 1) us += 3.6f + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
+            if (us < best.us) best = {t, sp, us};
+        }
+    }
+    if (want_split > 0) best.splits = want_split < steps ? want_split : steps;
+    return best;
+}
+static size_t partial_bytes(const SmPlan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
+static int strips_of(const SmPlan &z, int N) { return z.splits > 1 ? up(N, 32) : up(N, kSmTiles[z.tile].bm) * kSmTiles[z.tile].wm; }
+
+// Scratch of a pass, laid out in order.
+struct SmLayout {
+    bool half, laid;            // fp32; w is laid out
+    int isteps, piece, pieces;  // steps of memory of a row of x or w; classes of a piece, pieces
+    int products;               // of outputs and of dx, per step of memory
+    SmPlan z, dx, dw;           // of a whole piece
+    size_t x, w, xexp, wexp, least, top, label_out, dz, dz_dx, dxs, strips, partial, total;
+    SmLayout(const owt_fc_desc *d, int ol, bool forward)
     {
+        const int N = d->N, I = d->I;
+        half = d->dtype == OWT_F32;
+        isteps = up(I, 64);
+        laid = half || I % 64;
+        products = half ? SM_THREE : SM_ONE;
+        const size_t row = (size_t)isteps * (half ? 256 : 128);
+        piece = forward ? forward_piece(row, ol) : backward_piece(N, row, ol);
+        pieces = ol ? up(ol, piece) : 0;
+        z = sm_plan(N, piece, isteps * products, true);
+        if (forward && pieces > 1) z.splits = 1;        // (a split row's outputs are joined in one go)
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
-        z = take((size_t)d->N * (ol < kPiece ? ol : kPiece) * 4);
-        top = take(forward ? (size_t)d->N * 12 : 0);
-        dx = take(!forward ? (size_t)d->N * d->I * 4 : 0);
-        total = d->N ? at : 0;
+        const size_t rows = forward ? N : (size_t)up(N, 64) * 64;
+        x = take(!forward || laid ? rows * row : 0);
+        w = take(laid ? (size_t)piece * row : 0);
+        xexp = take(half ? (size_t)N * 4 : 0);
+        wexp = take(half ? (size_t)piece * 4 : 0);
+        least = take(half ? (size_t)(pieces + 1) * 4 : 0);
+        top = label_out = dz = dz_dx = dxs = strips = partial = total = 0;
+        dx = dw = z;
+        if (z.tile < 0) return;
+        size_t parts = partial_bytes(z, N, piece);
+        if (forward) {
+            top = take(z.splits > 1 ? 0 : (size_t)pieces * up(piece, kSmTiles[z.tile].bn) * kSmTiles[z.tile].wn * N * sizeof(Top));
+            label_out = take((size_t)N * 4);
+        } else {
+            const int psteps = up(piece, 64);
+            dx = sm_plan(N, I, psteps * (half ? SM_THREE : SM_ONE), true);
+            dw = sm_plan(piece, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), false);
+            dz = take((size_t)N * psteps * 256);
+            dz_dx = take(half ? (size_t)N * psteps * 256 : 0);
+            dxs = take(!half && pieces > 1 ? (size_t)N * I * 4 : 0);
+            strips = take((size_t)strips_of(z, N) * piece * 4);
+            const size_t a = partial_bytes(dx, N, I), b = partial_bytes(dw, piece, I);
+            parts = parts > a ? parts : a;
+            parts = parts > b ? parts : b;
+        }
+        partial = take(parts);
+        total = N ? at : 0;
+    }
+    bool fits() const { return z.tile >= 0 && dx.tile >= 0 && dw.tile >= 0; }
+    // Weights that are laid out go in pieces of at most 128 MB; outputs are not kept, so that the others are one piece.
+    int forward_piece(size_t row, int ol) const
+    {
+        if (!laid) return ol;
+        const size_t fit = ((size_t)128 << 20) / row / 256 * 256;
+        return fit < 256 ? (ol < 256 ? ol : 256) : fit < (size_t)ol ? (int)fit : ol;
+    }
+    int backward_piece(int N, size_t row, int ol) const
+    {
+        const size_t each = (size_t)N * (half ? 8 : 4) + (laid ? row : 0);
+        size_t fit = ((size_t)128 << 20) / (each ? each : 1) / 256 * 256;
+        fit = fit < 1024 ? 1024 : fit;
+        return fit < (size_t)ol ? (int)fit : ol;
     }
 };
 
-template <class TA, class TB, class TO> static void product(const SimpleProduct &p, hipStream_t s)
-{
-    const dim3 grid((unsigned)((p.N + 63) / 64), (unsigned)((p.M + 63) / 64));
-    hipLaunchKernelGGL((simple_product_kernel<TA, TB, TO>), grid, dim3(256), 0, s, p);
-}
-static unsigned groups_of(size_t n) { return (unsigned)((n + 255) / 256); }
+static owt_status check_fits(const SmLayout &l) { return l.fits() ? OWT_OK : fail(OWT_EUNSUPPORTED, "more work-groups than a launch holds"); }
 
-// outputs of classes [v0, v0 + cols)
-template <class T> static void outputs(const owt_fc_desc *d, const void *x, const void *w, const float *bias, int v0, int cols, float *z, hipStream_t s)
+static hipError_t launch(bool half, int product, int tile, const SmParams &p, hipStream_t s)
 {
-    const SimpleProduct p = {x, (const T *)w + (size_t)v0 * d->I, d->I, 1, d->I, 1, nullptr, 0, d->N, cols, d->I, bias ? bias + v0 : nullptr, 1.f, 0.f, z, cols};
-    product<T, T, float>(p, s);
+    const bool ends = product == SM_PRODUCT_TOP || product == SM_PRODUCT_DZ;
+    if (half) return ends ? owt_launch_softmax_half_ends(product, tile, p, s) : owt_launch_softmax_half_out(product, tile, p, s);
+    return ends ? owt_launch_softmax_bf16_ends(product, tile, p, s) : owt_launch_softmax_bf16_out(product, tile, p, s);
+}
+// Numbers the tiles of a product; a plan for a whole piece serves the last one, too.
+static void lay_tiles(SmParams &p, const SmPlan &pl)
+{
+    const SmTileCost &q = kSmTiles[pl.tile];
+    p.tiles_n = up(p.N, q.bn);
+    p.tiles = p.tiles_n * up(p.M, q.bm);
+    p.splits = pl.splits;
+    p.steps_per_split = up(p.steps / p.products, pl.splits) * p.products;
+}
+static unsigned groups_of(size_t n, size_t most = 1u << 22)
+{
+    const size_t g = (n + 255) / 256;
+    return (unsigned)(g < most ? g : most);
+}
+static void join_parts(bool half, const SmParams &p, hipStream_t s)
+{
+    const dim3 grid(groups_of((size_t)p.M * ((p.N + 3) / 4), 8192));
+    if (half) hipLaunchKernelGGL(sm_join_kernel<true>, grid, dim3(256), 0, s, p);
+    else hipLaunchKernelGGL(sm_join_kernel<false>, grid, dim3(256), 0, s, p);
+}
+static hipError_t results(bool half, int product, SmParams p, const SmPlan &pl, hipStream_t s)
+{
+    lay_tiles(p, pl);
+    const hipError_t e = launch(half, product, pl.tile, p, s);
+    if (e == hipSuccess && pl.splits > 1) join_parts(half, p, s);
+    return e;
 }
 
-template <class T>
-static owt_status forward(const owt_fc_desc *d, int ol, const void *x, const void *w, const float *bias, const int *labels, float *lse, float *target,
+static owt_status launched(hipError_t e = hipSuccess)
+{
+    if (e == hipSuccess) e = hipGetLastError();
+    return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
+}
+
+// x, or a piece of w, as operands of the products
+struct SmSource {
+    const owt_fc_desc *d;
+    const SmLayout &l;
+    char *ws;
+    hipStream_t s;
+
+    SmOperand along(const void *at, int rows) const
+    {
+        const int planes = l.half ? 2 : 1;
+        return {(const unsigned char *)at, (size_t)l.isteps * 128 * planes, (size_t)(128 * planes), rows, 0, planes};
+    }
+    static SmOperand across(const SmOperand &o, int rows, int steps)
+    {
+        return {o.at, o.ld, 64 * o.ld, rows, 8 * steps, o.planes};
+    }
+    void lay(SmPrep p) const
+    {
+        p.cols = d->I;
+        p.steps = l.isteps;
+        if (l.half) {
+            p.least = (int *)(ws + l.least);
+            const unsigned more = p.x_exps ? groups_of(p.x_rows, 64) : 0;
+            hipLaunchKernelGGL(sm_halves_kernel, dim3((unsigned)up(p.out_rows, 4) + more), dim3(256), 0, s, p);
+        } else hipLaunchKernelGGL(sm_rows_kernel, dim3(groups_of((size_t)p.out_rows * p.steps * 8, 8192)), dim3(256), 0, s, p);
+    }
+    // backward: rows without a class and those up to a whole step are zeros
+    SmOperand x(const void *from, const int *labels, bool forward) const
+    {
+        if (forward && !l.laid) return along(from, d->N);
+        SmPrep p;
+        memset(&p, 0, sizeof(p));
+        p.from = from;
+        p.to = (unsigned char *)(ws + l.x);
+        p.rows = d->N;
+        p.out_rows = forward ? d->N : up(d->N, 64) * 64;
+        p.labels = forward ? nullptr : labels;
+        p.classes = d->O_total;
+        p.exps = (int *)(ws + l.xexp);
+        p.leasts = l.pieces + 1;
+        p.piece = -1;
+        lay(p);
+        return along(ws + l.x, d->N);
+    }
+    SmOperand w(const void *from, int piece, int v0, int cols, const float *weight, bool forward) const
+    {
+        const char *at = (const char *)from + (size_t)v0 * d->I * (l.half ? 4 : 2);
+        if (!l.laid) return along(at, cols);
+        SmPrep p;
+        memset(&p, 0, sizeof(p));
+        p.from = at;
+        p.to = (unsigned char *)(ws + l.w);
+        p.rows = p.out_rows = cols;
+        p.exps = (int *)(ws + l.wexp);
+        p.piece = piece;
+        if (!forward && piece == 0) {
+            p.weight = weight;
+            p.x_exps = (const int *)(ws + l.xexp);
+            p.x_rows = d->N;
+        }
+        lay(p);
+        return along(ws + l.w, cols);
+    }
+};
+
+// outputs of a piece: what TOP, DZ and Z have in common
+static SmParams outputs(const owt_fc_desc *d, const SmLayout &l, char *ws, const SmOperand &x, const SmOperand &w, int ol, int v0, int cols, const float *bias,
+                        const int *labels)
+{
+    SmParams p;
+    memset(&p, 0, sizeof(p));
+    p.a = x;
+    p.b = w;
+    p.M = d->N;
+    p.N = cols;
+    p.products = l.products;
+    p.steps = l.isteps * l.products;
+    p.bias = bias ? bias + v0 : nullptr;
+    p.row_exp = (const int *)(ws + l.xexp);
+    p.col_exp = (const int *)(ws + l.wexp);
+    p.labels = labels;
+    p.classes = d->O_total;
+    p.off = d->rank * ol + v0;
+    p.alpha = 1.f;
+    p.partial = (float *)(ws + l.partial);
+    lay_tiles(p, l.z);
+    return p;
+}
+
+static owt_status forward(const owt_fc_desc *d, const SmLayout &l, int ol, const void *x, const void *w, const float *bias, const int *labels, float *lse, float *target,
                           float *loss, char *ws, hipStream_t s)
 {
-    const SoftmaxLayout l(d, ol, true);
-    float *z = (float *)(ws + l.z), *at = target ? target : (float *)(ws + l.top) + 2 * (size_t)d->N;
-    Top *top = (Top *)(ws + l.top);
-    for (int v0 = 0; v0 < ol; v0 += kPiece) {
-        const int cols = ol - v0 < kPiece ? ol - v0 : kPiece;
-        outputs<T>(d, x, w, bias, v0, cols, z, s);
-        hipLaunchKernelGGL(piece_top_kernel, dim3((unsigned)((d->N + 3) / 4)), dim3(256), 0, s, z, d->N, cols, d->rank * ol + v0, labels, d->O_total, v0 == 0,
-                           top, at);
+    const SmSource from{d, l, ws, s};
+    const SmOperand xo = from.x(x, nullptr, true);
+    SmRows r = {(const Top *)(ws + l.top), 0, d->N, (const float *)(ws + l.label_out), labels, d->O_total, d->rank * ol, ol, lse, target, loss};
+    for (int k = 0; k < l.pieces; k++) {
+        const int v0 = k * l.piece, cols = ol - v0 < l.piece ? ol - v0 : l.piece;
+        const SmOperand wo = from.w(w, k, v0, cols, nullptr, true);
+        SmParams p = outputs(d, l, ws, xo, wo, ol, v0, cols, bias, labels);
+        p.target = (float *)(ws + l.label_out);
+        p.top = (Top *)(ws + l.top) + (size_t)r.parts * d->N;
+        if (p.splits > 1) {
+            const hipError_t e = launch(l.half, SM_PRODUCT_Z, l.z.tile, p, s);
+            if (e != hipSuccess) return launched(e);
+            if (l.half) hipLaunchKernelGGL(sm_split_top_kernel<true>, dim3((unsigned)d->N), dim3(256), 0, s, p, r);
+            else hipLaunchKernelGGL(sm_split_top_kernel<false>, dim3((unsigned)d->N), dim3(256), 0, s, p, r);
+            return launched();
+        }
+        const hipError_t e = launch(l.half, SM_PRODUCT_TOP, l.z.tile, p, s);
+        if (e != hipSuccess) return launched(e);
+        r.parts += p.tiles_n * kSmTiles[l.z.tile].wn;
     }
-    hipLaunchKernelGGL(lse_kernel, dim3(groups_of(d->N)), dim3(256), 0, s, d->N, top, labels, d->O_total, lse, at, loss);
+    if (d->N > 1024) hipLaunchKernelGGL(sm_finish_kernel<8>, dim3((unsigned)up(d->N, 32)), dim3(256), 0, s, r);
+    else hipLaunchKernelGGL(sm_finish_kernel<256>, dim3((unsigned)d->N), dim3(256), 0, s, r);
     return launched();
 }
 
-template <class T>
-static owt_status backward(const owt_fc_desc *d, int ol, const void *x, const void *w, const float *bias, const int *labels, const float *lse,
+static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, const void *x, const void *w, const float *bias, const int *labels, const float *lse,
                            const float *weight, float alpha, float beta, void *dx, float *dw, float *db, char *ws, hipStream_t s)
 {
-    const SoftmaxLayout l(d, ol, false);
-    float *z = (float *)(ws + l.z), *dxs = (float *)(ws + l.dx);
-    for (int v0 = 0; v0 < ol; v0 += kPiece) {
-        const int cols = ol - v0 < kPiece ? ol - v0 : kPiece;
-        if (d->N) {
-            outputs<T>(d, x, w, bias, v0, cols, z, s);
-            hipLaunchKernelGGL(piece_dz_kernel, dim3(groups_of((size_t)d->N * cols)), dim3(256), 0, s, z, d->N, cols, d->rank * ol + v0, labels, d->O_total, lse, weight);
+    SmParams none;
+    memset(&none, 0, sizeof(none));
+    if (d->N == 0) {            // sums of nothing
+        none.M = ol;
+        none.N = d->I;
+        none.alpha = alpha;
+        none.beta = beta;
+        none.out = dw;
+        join_parts(false, none, s);
+        if (db) {
+            none.N = 1;
+            none.out = db;
+            join_parts(false, none, s);
         }
-        if (dx && d->N)
-            product<float, T, float>({z, (const T *)w + (size_t)v0 * d->I, cols, 1, 1, d->I, nullptr, 0, d->N, d->I, cols, nullptr, 1.f, v0 ? 1.f : 0.f, dxs, d->I}, s);
-        product<float, T, float>({z, x, 1, cols, 1, d->I, labels, d->O_total, cols, d->I, d->N, nullptr, alpha, beta, dw + (size_t)v0 * d->I, d->I}, s);
-        if (db) hipLaunchKernelGGL(piece_dbias_kernel, dim3(groups_of(cols)), dim3(256), 0, s, z, d->N, cols, alpha, beta, db + v0);
+        return launched();
     }
-    if (dx && d->N) {
-        const size_t n = (size_t)d->N * d->I;
-        hipLaunchKernelGGL(store_rows_kernel<T>, dim3(groups_of(n)), dim3(256), 0, s, dxs, n, d->I, labels, d->O_total, (T *)dx);
+    const SmSource from{d, l, ws, s};
+    const SmOperand xo = from.x(x, labels, false);
+    const int products = l.half ? SM_THREE : SM_PAIR, nsteps = up(d->N, 64);
+    int *least = (int *)(ws + l.least);
+    for (int k = 0; k < l.pieces; k++) {
+        const int v0 = k * l.piece, cols = ol - v0 < l.piece ? ol - v0 : l.piece, psteps = up(cols, 64);
+        const SmOperand wo = from.w(w, k, v0, cols, weight, false);
+        SmParams p = outputs(d, l, ws, xo, wo, ol, v0, cols, bias, labels);
+        p.lse = lse;
+        p.weight = weight;
+        p.dz = (unsigned char *)(ws + l.dz);
+        p.dz_dx = (unsigned char *)(ws + l.dz_dx);
+        p.dz_ld = (size_t)psteps * 256;
+        p.least_x = least;
+        p.least_w = least + 1 + k;
+        p.dbias = db ? (float *)(ws + l.strips) : nullptr;
+        hipError_t e = launch(l.half, p.splits > 1 ? SM_PRODUCT_Z : SM_PRODUCT_DZ, l.z.tile, p, s);
+        if (e != hipSuccess) return launched(e);
+        if (p.splits > 1) {
+            const dim3 grid((unsigned)psteps, (unsigned)up(d->N, 32));
+            if (l.half) hipLaunchKernelGGL(sm_split_dz_kernel<true>, grid, dim3(256), 0, s, p);
+            else hipLaunchKernelGGL(sm_split_dz_kernel<false>, grid, dim3(256), 0, s, p);
+        }
+        if (db) hipLaunchKernelGGL(sm_dbias_kernel, dim3(groups_of(cols)), dim3(256), 0, s, p.dbias, strips_of(l.z, d->N), cols, alpha, beta, db + v0);
+
+        if (dx) {
+            SmParams q = none;
+            q.a = {l.half ? p.dz_dx : p.dz, p.dz_ld, 256, d->N, 0, 2};
+            q.b = SmSource::across(wo, cols, l.isteps);
+            q.M = d->N;
+            q.N = d->I;
+            q.products = l.half ? SM_THREE : SM_ONE;
+            q.steps = psteps * q.products;
+            q.labels = labels;
+            q.classes = d->O_total;
+            q.weight = weight;
+            q.alpha = 1.f;
+            q.least = p.least_w;
+            q.partial = p.partial;
+            float *sums = l.half ? (float *)dx : (float *)(ws + l.dxs);
+            const bool last = k == l.pieces - 1;
+            q.add = k ? sums : nullptr;
+            q.out = last ? dx : sums;
+            q.bf16 = last && !l.half;
+            if ((e = results(l.half, SM_PRODUCT_DX, q, l.dx, s)) != hipSuccess) return launched(e);
+        }
+        SmParams q = none;
+        q.a = {p.dz, p.dz_ld, 64 * p.dz_ld, d->N, 8 * psteps, 2};
+        q.b = SmSource::across(xo, nsteps * 64, l.isteps);
+        q.M = cols;
+        q.N = d->I;
+        q.products = products;
+        q.steps = nsteps * products;
+        q.alpha = alpha;
+        q.beta = beta;
+        q.least = least;
+        q.partial = p.partial;
+        q.out = dw + (size_t)v0 * d->I;
+        if ((e = results(l.half, SM_PRODUCT_DW, q, l.dw, s)) != hipSuccess) return launched(e);
     }
     return launched();
 }
@@ -280,7 +696,9 @@ size_t owt_fc_softmax_workspace_bytes(const owt_fc_desc *d, int pass)
     int ol;
     if (pass < 0 || pass > 2) { fail(OWT_EINVAL, "pass must be 0, 1 or 2"); return (size_t)-1; }
     if (check_softmax(d, ol) != OWT_OK) return (size_t)-1;
-    return SoftmaxLayout(d, ol, pass == OWT_PASS_FWD).total;
+    const SmLayout l(d, ol, pass == OWT_PASS_FWD);
+    if (check_fits(l) != OWT_OK) return (size_t)-1;
+    return l.total;
 }
 
 owt_status owt_fc_softmax_fwd(const owt_fc_desc *d, const void *x, const void *w, const float *bias, const int *labels_or_null, float *lse,
@@ -294,11 +712,12 @@ owt_status owt_fc_softmax_fwd(const owt_fc_desc *d, const void *x, const void *w
     OWT_TRY(need_ptr(x, "x")); OWT_TRY(need_ptr(w, "w")); OWT_TRY(need_ptr(lse, "lse"));
     if (d->flags & OWT_BIAS) OWT_TRY(need_ptr(bias, "bias"));
     OWT_TRY(may_ptr(labels_or_null, "labels")); OWT_TRY(may_ptr(target_or_null, "target")); OWT_TRY(may_ptr(loss_or_null, "loss"));
-    OWT_TRY(need_ws(ws, ws_bytes, SoftmaxLayout(d, ol, true).total));
+    const SmLayout l(d, ol, true);
+    OWT_TRY(check_fits(l));
+    OWT_TRY(need_ws(ws, ws_bytes, l.total));
     const float *b = (d->flags & OWT_BIAS) ? bias : nullptr;
     hipStream_t s = (hipStream_t)hip_stream;
-    if (d->dtype == OWT_BF16) return forward<bf16_t>(d, ol, x, w, b, labels_or_null, lse, target_or_null, loss_or_null, (char *)ws, s);
-    return forward<float>(d, ol, x, w, b, labels_or_null, lse, target_or_null, loss_or_null, (char *)ws, s);
+    return forward(d, l, ol, x, w, b, labels_or_null, lse, target_or_null, loss_or_null, (char *)ws, s);
 }
 
 owt_status owt_softmax_join(int workers, int N, int classes, const float *lses, const float *targets, const int *labels, float *lse,
@@ -326,12 +745,12 @@ owt_status owt_fc_softmax_bwd(const owt_fc_desc *d, const void *x, const void *w
         if (d->flags & OWT_BIAS) OWT_TRY(need_ptr(bias, "bias"));
         OWT_TRY(may_ptr(weight_or_null, "weight"));
     }
-    OWT_TRY(need_ws(ws, ws_bytes, SoftmaxLayout(d, ol, false).total));
+    const SmLayout l(d, ol, false);
+    OWT_TRY(check_fits(l));
+    OWT_TRY(need_ws(ws, ws_bytes, l.total));
     const float *b = (d->flags & OWT_BIAS) ? bias : nullptr;
     hipStream_t s = (hipStream_t)hip_stream;
-    if (d->dtype == OWT_BF16)
-        return backward<bf16_t>(d, ol, x, w, b, labels, lse, weight_or_null, alpha, beta, dx_partial_or_null, dw, dbias_or_null, (char *)ws, s);
-    return backward<float>(d, ol, x, w, b, labels, lse, weight_or_null, alpha, beta, dx_partial_or_null, dw, dbias_or_null, (char *)ws, s);
+    return backward(d, l, ol, x, w, b, labels, lse, weight_or_null, alpha, beta, dx_partial_or_null, dw, dbias_or_null, (char *)ws, s);
 }
 
 }  // extern "C"

@@ -1,0 +1,49 @@
+// Instantiations of smgemm.hpp: -DOWT_INST_HALF=0 (bf16) or 1 (f16), -DOWT_INST_OUT=0 (outputs as statistics or dz) or 1 (stored sums).
+#include "softmax.hpp"
+
+namespace owt {
+
+#if OWT_INST_HALF
+typedef SmHalf Op;
+#else
+typedef SmBf16 Op;
+#endif
+
+template <bool TA, bool TB, class S, int END> static hipError_t go(const SmParams &p, hipStream_t s)
+{
+    hipLaunchKernelGGL((sm_kernel<Op, TA, TB, S, END>), dim3((unsigned)owt_split_major_grid(p.tiles, p.splits)), dim3(64 * S::NW), 0, s, p);
+    return hipGetLastError();
+}
+template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmParams &p, hipStream_t s)
+{
+    if (tile == SM_BIG) return go<TA, TB, SmBig, END>(p, s);
+    if (tile == SM_MID) return go<TA, TB, SmMid, END>(p, s);
+    if (tile == SM_SMALL) return go<TA, TB, SmSmall, END>(p, s);
+    if constexpr (!TA) return go<TA, TB, SmFew, END>(p, s);
+    return hipErrorInvalidValue;
+}
+
+#if OWT_INST_HALF && OWT_INST_OUT
+#define OWT_INST_NAME owt_launch_softmax_half_out
+#elif OWT_INST_HALF
+#define OWT_INST_NAME owt_launch_softmax_half_ends
+#elif OWT_INST_OUT
+#define OWT_INST_NAME owt_launch_softmax_bf16_out
+#else
+#define OWT_INST_NAME owt_launch_softmax_bf16_ends
+#endif
+
+hipError_t OWT_INST_NAME(int product, int tile, const SmParams &p, hipStream_t s)
+{
+#if OWT_INST_OUT
+    if (product == SM_PRODUCT_Z) return tiled<false, false, SM_OUT>(tile, p, s);
+    if (product == SM_PRODUCT_DX) return tiled<false, true, SM_OUT>(tile, p, s);
+    if (product == SM_PRODUCT_DW) return tiled<true, true, SM_OUT>(tile, p, s);
+#else
+    if (product == SM_PRODUCT_TOP) return tiled<false, false, SM_TOP>(tile, p, s);
+    if (product == SM_PRODUCT_DZ) return tiled<false, false, SM_DZ>(tile, p, s);
+#endif
+    return hipErrorInvalidValue;
+}
+
+}  // namespace owt

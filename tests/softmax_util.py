@@ -44,11 +44,18 @@ class Reference:
             self.target = np.where(self.real, np.where(self.mine, self.z[np.arange(len(x)), self.at], -np.inf), 0.0)
             self.loss = np.where(self.real, np.where(np.isneginf(self.target), np.inf, self.lse - self.target), 0.0)
 
+    def floors(self):
+        """fp32 operands in two f16 values: a row's largest magnitude is at 2^14 or above, the second value's smallest step is 2^-24, half of it 2^-25: no value is off by
+        more than 2^-39 of its row's largest, however small it is itself."""
+        return tuple(np.abs(a).max(1, keepdims=True) for a in (self.x, self.w))
+
     def z_off(self):
         """How far an output may be off: operands in two f16 values lose 2^-22 of each (and the product of what is second, 2^-22), sums of I products and the
         bias in fp32, in any order and with each product or sum cut instead of rounded, 2 U a step."""
         size = np.abs(self.x) @ np.abs(self.w).T + np.where(np.isfinite(self.b), np.abs(self.b), 0.0)
-        return (3 * 2.0 ** -22 + 2 * U * (self.x.shape[1] + 2)) * size
+        mx, mw = self.floors()
+        floor = 2.0 ** -39 * (mx * np.abs(self.w).sum(1)[None, :] + np.abs(self.x).sum(1)[:, None] * mw.T)
+        return (3 * 2.0 ** -22 + 2 * U * (self.x.shape[1] + 2)) * size + floor
 
     def lse_off(self):
         """The log of a sum of exponentials moves by no more than its largest argument does; each exponential is good to 2^-20 of itself (its argument, up to 87 in
@@ -63,7 +70,8 @@ class Reference:
         d[np.arange(len(d))[self.mine], self.at[self.mine]] -= 1.0
         f = np.where(self.real, 1.0 if weight is None else weight.astype(np.float64), 0.0)[:, None]
         # an output's error, the rounding of the difference and of the exponential itself, then of dz
-        off = p * np.expm1(self.z_off() + 2 * U * np.abs(lse)[:, None] + 2.0 ** -17) + 4 * U * np.abs(d)
+        # (an exponential below 2^-126, the smallest normal number, and what is second of a value below 2^-117, may come out as zero: off by 2^-126 each)
+        off = 2.0 ** -125 + p * np.expm1(self.z_off() + 2 * U * np.abs(lse)[:, None] + 2.0 ** -17) + 4 * U * np.abs(d)
         return d * f, off * np.abs(f)
 
 
@@ -74,10 +82,21 @@ def grads(ref, lse, weight, dt, alpha, beta, dw0, db0):
     second = planes_error(dt)
     aw, ax = np.abs(ref.w), np.abs(ref.x)
     one = 2.0 ** -8 if dt == "bf16" else second
+    # dz in two f16 values is at 2^15 for 1 under one power of two: off by 2^-25 under it, 2^-40 without.  For dw a row n of dz comes times 2^-e, e of x's row, times the weight,
+    # and the power of two is the largest such factor's or up to twice that; 2^-e is x's largest magnitude over 2^14 .. 2^15: the row's 2^-40 is that times the largest row's
+    # weight times magnitude over this row's magnitude, times 4.  For dx the same with w's rows and no weight.  x and w have floors of their own.
+    mx, mw = ref.floors()
+    wt = np.where(ref.real, 1.0 if weight is None else np.abs(weight.astype(np.float64)), 0.0)[:, None]
+    with np.errstate(all="ignore"):
+        rx = np.where(mx > 0, 4 * (wt * mx).max(initial=0.0) / mx, 0.0)
+        rw = np.where(mw > 0, 4 * mw.max() / mw, 0.0)
+    low_x, low_w = 2.0 ** -40 * rx + 0 * ax, 2.0 ** -40 * rw + 0 * aw
+    low_dw = (low_x * ax).sum(0)[None, :] + 2.0 ** -39 * (np.abs(dz).T @ (mx + 0 * ax)) if dt == "f32" else 0.0
+    low_dx = wt * (low_w * aw).sum(0)[None, :] + 2.0 ** -39 * (np.abs(dz) @ (mw + 0 * aw)) if dt == "f32" else 0.0
     dx = dz @ ref.w
-    dx_off = (off + np.abs(dz) * (one + second + 2 * U * (O + 2))) @ aw + np.abs(dx) * (2.0 ** -8 if dt == "bf16" else U)
+    dx_off = (off + np.abs(dz) * (one + second + 2 * U * (O + 2))) @ aw + np.abs(dx) * (2.0 ** -8 if dt == "bf16" else U) + low_dx
     dw = alpha * (dz.T @ ref.x) + (beta * dw0.astype(np.float64) if beta else 0.0)
-    dw_off = abs(alpha) * ((off + np.abs(dz) * (2 * second + 2 * U * (N + 2))).T @ ax) + 4 * U * np.abs(dw) + (2 * U * np.abs(beta * dw0) if beta else 0.0)
+    dw_off = abs(alpha) * ((off + np.abs(dz) * (2 * second + 2 * U * (N + 2))).T @ ax) + 4 * U * np.abs(dw) + (2 * U * np.abs(beta * dw0) if beta else 0.0) + abs(alpha) * low_dw
     db = alpha * dz.sum(0) + (beta * db0.astype(np.float64) if beta else 0.0)
     db_off = abs(alpha) * (off + np.abs(dz) * 2 * U * (N + 2)).sum(0) + 4 * U * np.abs(db) + (2 * U * np.abs(beta * db0) if beta else 0.0)
     return dict(dx=(dx, dx_off), dw=(dw, dw_off), db=(db, db_off))

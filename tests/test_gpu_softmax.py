@@ -316,3 +316,43 @@ def test_two_calls_at_once_on_streams_of_their_own():
     torch.cuda.synchronize()
     for c in calls:
         assert all(torch.equal(p, q) for p, q in zip(*c["o"]))
+
+
+# ------------------------------------------------------------------------------------------------ every tile, and sums that are split
+
+TILES = {"256x256": 120, "128x128": 121, "64x64": 122, "32x256": 123}
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("N,I,O", [(5, 130, 70), (300, 256, 600), (520, 72, 1030), (129, 1024, 257)])
+def test_tiles_and_splits(N, I, O, tile, splits, dt):
+    from gpu_util import force
+    x, w, b, labels, weight = inputs(N, I, O, N + I, dt)
+    ref = Reference(x, w, b, labels)
+    l32 = ref.lse.astype(np.float32)
+    g = np.random.default_rng(3)
+    dw0, db0 = g.standard_normal((O, I)).astype(np.float32), g.standard_normal(O).astype(np.float32)
+    with force(TILES[tile], splits):
+        lse, target, loss = run_fwd(N, I, O, dt, x, w, b, labels)
+        got = run_bwd(N, I, O, dt, x, w, b, labels, l32, weight, 1.0 / N, 0.5, dw0, db0)
+    assert_within(lse, ref.lse, ref.lse_off(), "lse")
+    assert_within(target, ref.target, ref.z_off().max(1), "target")
+    assert_within(loss, ref.loss, ref.lse_off() + ref.z_off().max(1), "loss")
+    for k, (want, off) in grads(ref, l32, weight, dt, 1.0 / N, 0.5, dw0, db0).items():
+        assert_within(got[k], want, off, k)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_pieces(dt):
+    """So many rows that the classes are taken in pieces, the last of them short; few values of x, so that the reference is quick."""
+    N, I, O = 20000, 8, 3000
+    x, w, b, labels, weight = inputs(N, I, O, 40, dt)
+    ref = Reference(x, w, b, labels)
+    l32 = ref.lse.astype(np.float32)
+    lse, _, _ = run_fwd(N, I, O, dt, x, w, b, labels)
+    assert_within(lse, ref.lse, ref.lse_off(), "lse")
+    got = run_bwd(N, I, O, dt, x, w, b, labels, l32, weight, 1.0 / N, 0.0, None, None)
+    for k, (want, off) in grads(ref, l32, weight, dt, 1.0 / N, 0.0, None, None).items():
+        assert_within(got[k], want, off, k)
