@@ -56,6 +56,11 @@ __global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep p)
     }
 }
 
+// Every work-group has a word to say, and hardly any a new one: the others only look (4096 atomics on one word took 50 us).
+__device__ __forceinline__ void lower(int *least, int v)
+{
+    if (v < __hip_atomic_load(least, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(least, v);
+}
 __device__ __forceinline__ int least_of_wave(int v)
 {
 #pragma unroll
@@ -76,7 +81,7 @@ __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
             if (p.x_exps[n] != kSmNone && g > 0.f && __builtin_isfinite(g)) least = min(least, p.x_exps[n] - (ilogbf(g) + 1));
         }
         least = least_of_wave(least);
-        if (lane == 0) atomicMin(p.least, least);
+        if (lane == 0) lower(p.least, least);
         return;
     }
     if (p.leasts && blockIdx.x == 0)        // x: before anything looks for them
@@ -117,7 +122,7 @@ __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
         __shared__ int part[4];
         if (lane == 0) part[wave] = exp;
         __syncthreads();
-        if (threadIdx.x == 0) atomicMin(p.least + 1 + p.piece, min(min(part[0], part[1]), min(part[2], part[3])));
+        if (threadIdx.x == 0) lower(p.least + 1 + p.piece, min(min(part[0], part[1]), min(part[2], part[3])));
     }
 }
 
@@ -201,11 +206,11 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_dz_kernel
     const size_t whole = (size_t)p.M * p.N;
     const SmDzColumns k = sm_dz_columns<SCALED>(p, c);
     float sums[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int m = blockIdx.y * 32 + r; m < min(p.M, (int)blockIdx.y * 32 + 32); m += 16) {
+    for (int m = blockIdx.y * 32 + r; m < (int)blockIdx.y * 32 + 32; m += 16) {      // (rows past the last are zeros; nothing is read or written of them)
         float z[4] = {0.f, 0.f, 0.f, 0.f};
         const float *row = p.partial + (size_t)m * p.N + c;
         if ((p.N & 3) == 0) {
-            if (c < p.N)
+            if (c < p.N && m < p.M)
 #pragma unroll 4
                 for (int s = 0; s < p.splits; s++) {
                     const float4 v = *(const float4 *)(row + s * whole);
@@ -215,8 +220,8 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_dz_kernel
             for (int s = 0; s < p.splits; s++)
 #pragma unroll
                 for (int t = 0; t < 4; t++)
-                    if (c + t < p.N) z[t] += row[s * whole + t];
-        sm_dz<SCALED>(p, m, c, make_float4(z[0], z[1], z[2], z[3]), sm_dz_row<SCALED>(p, m), k, sums);
+                    if (c + t < p.N && m < p.M) z[t] += row[s * whole + t];
+        sm_dz<SCALED, false>(p, m, c, make_float4(z[0], z[1], z[2], z[3]), sm_dz_row<SCALED>(p, m), k, sums);
     }
     if (!p.dbias) return;
     part[r][q] = make_float4(sums[0], sums[1], sums[2], sums[3]);

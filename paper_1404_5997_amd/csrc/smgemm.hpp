@@ -126,7 +126,7 @@ enum { SM_TOP, SM_DZ, SM_OUT };
 
 template <int WM_, int WN_, int MB_, int NB_, int NS_, int OCC_> struct SmShape {
     static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, NS = NS_, OCC = OCC_, NW = WM * WN, BM = 32 * MB * WM, BN = 32 * NB * WN;
-    static constexpr int STAGE = (BM + BN) * 128, LDS = NS * STAGE;
+    static constexpr int STAGE = (BM + BN) * 128, RING = NS * STAGE, LDS = RING + (BM + BN) * 4;
 };
 
 // The pieces of a tile of R rows of C that a lane loads, and where a fragment's lane reads.
@@ -147,16 +147,17 @@ template <bool ACROSS, int R, int NW> struct SmTile {
 };
 
 // dz = weight (exp(z - lse) - [label]): what a row and four columns bring to it, and what is kept.  Rows without a class are zeros, and so are
-// columns past the last up to a whole step.
+// columns past the last up to a whole step: an lse of infinity and a bias of -infinity take exponentials to zero.  (Rows all of whose outputs are -infinity
+// have an lse of -infinity: any other number will do in its place.)
 struct SmDzRow { float lse, weight; int label, exp; };      // exp: of x's row
 struct SmDzColumns { float bias[4]; int exp[4]; };          // exp: of w's rows
-constexpr int kSmNoLabel = -0x7fffffff;         // (a row that counts has at least -2^31 / 2 here)
 template <bool SCALED> __device__ __forceinline__ SmDzRow sm_dz_row(const SmParams &p, int m)
 {
     const int at = m < p.M ? p.labels[m] : -1;
-    if (m >= p.M || !has_class(at, p.classes)) return {0.f, 0.f, kSmNoLabel, 0};
+    if (m >= p.M || !has_class(at, p.classes)) return {INFINITY, 0.f, -1, 0};
+    const float lse = p.lse[m];
     // (a label behind these columns is no column of the last step's zeros, either)
-    return {p.lse[m], p.weight ? p.weight[m] : 1.f, at - p.off < p.N ? at - p.off : -1, SCALED ? p.row_exp[m] : 0};
+    return {lse == -INFINITY ? 0.f : lse, p.weight ? p.weight[m] : 1.f, at - p.off < p.N ? at - p.off : -1, SCALED ? p.row_exp[m] : 0};
 }
 template <bool SCALED> __device__ __forceinline__ SmDzColumns sm_dz_columns(const SmParams &p, int c)
 {
@@ -192,17 +193,23 @@ __device__ __forceinline__ void sm_put_bf16s(unsigned char *to, const float (&v)
     *(uint2 *)to = hi;
     *(uint2 *)(to + 128) = make_uint2(f32x2_to_bf16x2(lo[0], lo[1]), f32x2_to_bf16x2(lo[2], lo[3]));
 }
-template <bool SCALED>
+// STARTED: sums that began at bias - lse / 2.  All lanes of a wavefront come here together.
+template <bool SCALED, bool STARTED>
 __device__ __forceinline__ void sm_dz(const SmParams &p, int m, int c, const float4 &sum, const SmDzRow &w, const SmDzColumns &k, float (&sums)[4])
 {
     const float u[4] = {sum.x, sum.y, sum.z, sum.w};
     float d[4], e[4];
 #pragma unroll
     for (int t = 0; t < 4; t++) {
-        const float z = (SCALED ? ldexpf(u[t], -(w.exp + k.exp[t])) : u[t]) + k.bias[t];
-        const float x = z == -INFINITY ? 0.f : exp_of(z - w.lse);
-        e[t] = w.label == kSmNoLabel ? 0.f : w.label == c + t ? x - 1.f : x;
-        d[t] = w.label == kSmNoLabel ? 0.f : w.weight * e[t];
+        const float from_lse = STARTED ? u[t] - 0.5f * w.lse : (SCALED ? ldexpf(u[t], -(w.exp + k.exp[t])) : u[t]) + k.bias[t] - w.lse;
+        e[t] = exp_of(from_lse);
+    }
+    if (__any((unsigned)(w.label - c) < 4u))        // (of many classes hardly ever)
+#pragma unroll
+        for (int t = 0; t < 4; t++) e[t] = w.label == c + t ? e[t] - 1.f : e[t];
+#pragma unroll
+    for (int t = 0; t < 4; t++) {
+        d[t] = w.weight * e[t];
         sums[t] += d[t];
     }
     if (m >= p.M || c >= (p.N + 63) / 64 * 64) return;
@@ -218,6 +225,8 @@ __device__ __forceinline__ void sm_dz(const SmParams &p, int m, int c, const flo
         sm_put_halves(p.dz_dx + at, e);
     } else sm_put_bf16s(p.dz + at, d);
 }
+
+struct __attribute__((packed, aligned(2))) SmFourHalves { uint32_t lo, hi; };
 
 // A result from its sum
 template <bool SCALED> __device__ __forceinline__ void sm_result(float (&v)[4], int shift, float factor, float alpha)
@@ -310,13 +319,50 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
         return sm_i32x4{l[0], l[1], h[0], h[1]};
     };
 
-    sm_f32x16 acc[MB][NB];
+    const bool some = END != SM_OUT || nst > 0;     // (split sums alone may have none here)
+    if (some)
 #pragma unroll
-    for (int i = 0; i < MB; i++)
+        for (int s = 0; s < NS; s++) {
+            aim(s_beg + s, s);
+#pragma unroll
+            for (int i = 0; i < L; i++) load(i);
+        }
+
+    // Sums of outputs in bf16 start at what is added to them anyhow, while the first operands are on their way: the columns' bias (-infinity for those that
+    // do not exist), and for dz less half of the rows' lse.  A sum's roundings go by its size on the way: of an output near lse, whose dz is a small difference, it
+    // runs from -lse / 2 to lse / 2 then and is rounded half as coarsely.
+    constexpr bool SCALED = std::is_same<Op, SmHalf>::value, STARTED = !SCALED && END != SM_OUT;
+    sm_f32x16 acc[MB][NB];
+    if (STARTED) {
+        float *bias = (float *)(lds + S::RING), *half = bias + BN;      // (each read from memory once, and not by every lane for itself: 45 us of 250 in a launch of 512 tiles)
+        for (int c = tid; c < BN; c += 64 * NW) bias[c] = n0 + c < p.N ? (p.bias ? p.bias[n0 + c] : 0.f) : -INFINITY;
+        if (END == SM_DZ)
+            for (int r = tid; r < BM; r += 64 * NW) half[r] = 0.5f * sm_dz_row<false>(p, m0 + r).lse;
+        __syncthreads();
+        float less[MB];
+#pragma unroll
+        for (int i = 0; i < MB; i++) less[i] = END == SM_DZ ? half[wm0 + 32 * i + li] : 0.f;
 #pragma unroll
         for (int j = 0; j < NB; j++)
 #pragma unroll
-            for (int r = 0; r < 16; r++) acc[i][j][r] = 0;
+            for (int g = 0; g < 4; g++) {
+                const float4 b = *(const float4 *)(bias + wn0 + 32 * j + 8 * g + 4 * lh);
+#pragma unroll
+                for (int i = 0; i < MB; i++) {
+                    acc[i][j][4 * g] = b.x - less[i];
+                    acc[i][j][4 * g + 1] = b.y - less[i];
+                    acc[i][j][4 * g + 2] = b.z - less[i];
+                    acc[i][j][4 * g + 3] = b.w - less[i];
+                }
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < MB; i++)
+#pragma unroll
+            for (int j = 0; j < NB; j++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[i][j][r] = 0;
+    }
 
     // A slice of 16 k: its products, and between them the reads of the next slice's fragments and, in a step's last one, loads.  The order is
     // kept as written: the compiler would gather the reads in front of the products that wait for them.
@@ -349,18 +395,13 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     // s_waitcnt vmcnt(n) lgkmcnt(0), expcnt untouched; then the same of all wavefronts
 #define OWT_ARRIVED(n) do { asm volatile("" ::: "memory"); __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4)); \
                             __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); } while (0)
-    if (nst > 0) {
-#pragma unroll
-        for (int s = 0; s < NS; s++) {
-            aim(s_beg + s, s);
-#pragma unroll
-            for (int i = 0; i < L; i++) load(i);
-        }
-        OWT_ARRIVED((NS - 1) * L);
+    if (some) {
+        OWT_ARRIVED(STARTED ? 0 : (NS - 1) * L);    // (with what the sums started from, everything)
 #pragma unroll
         for (int f = 0; f < MB + NB; f++) read(0, 0, 0, f);
         int cur = 0;                                // stage s lives in buffer s % NS
-        for (int s = 0; s < nst; s++) {
+        int s = 0;
+        do {
             const int next = cur == NS - 1 ? 0 : cur + 1;
 #pragma unroll
             for (int kc = 0; kc < 3; kc++) slice(kc & 1, kc + 1, cur, 0);
@@ -370,7 +411,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
             aim(s_beg + s + NS, cur);
             slice(1, 0, next, L);
             cur = next;
-        }
+        } while (++s < nst);
     }
     __builtin_amdgcn_s_waitcnt(0x0F70);             // vmcnt(0): the last loads into LDS have landed, too
 #undef OWT_ARRIVED
@@ -378,14 +419,13 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
 
     // Accumulator register r of lane (li, lh): column 8 (r / 4) + 4 lh + r % 4 of C, row li of its block (the operands change places in the
     // instruction): four neighbouring results a lane.
-    constexpr bool SCALED = std::is_same<Op, SmHalf>::value;
     if constexpr (END == SM_TOP) {
         // Columns that do not exist have a bias of -infinity.  A lane has half of a row's values of its wavefront, the lane 32 away the other half.
         float *bias = (float *)lds;
         int *label = (int *)(bias + BN), *cexp = label + BM, *rexp = cexp + BN;
-        for (int c = tid; c < BN; c += 64 * NW) {
+        if (SCALED) for (int c = tid; c < BN; c += 64 * NW) {
             bias[c] = n0 + c < p.N ? (p.bias ? p.bias[n0 + c] : 0.f) : -INFINITY;
-            if (SCALED) cexp[c] = n0 + c < p.N ? -p.col_exp[n0 + c] : -kSmNone;      // (what is there is a copy of the last column)
+            cexp[c] = n0 + c < p.N ? -p.col_exp[n0 + c] : -kSmNone;      // (what is there is a copy of the last column)
         }
         for (int r = tid; r < BM; r += 64 * NW) {
             label[r] = m0 + r < p.M && p.labels && has_class(p.labels[m0 + r], p.classes) ? p.labels[m0 + r] - p.off - n0 : -1;
@@ -402,21 +442,29 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
 #pragma unroll
                     for (int g = 0; g < 4; g++) {
                         const int c = 32 * j + 8 * g;
-                        const float4 b4 = *(const float4 *)(bias + wn0 + c + 4 * lh);
-                        const float b[4] = {b4.x, b4.y, b4.z, b4.w};
-                        int e[4] = {0, 0, 0, 0};
                         if (SCALED) {
+                            const float4 b4 = *(const float4 *)(bias + wn0 + c + 4 * lh);
                             const int4 e4 = *(const int4 *)(cexp + wn0 + c + 4 * lh);
-                            e[0] = e4.x; e[1] = e4.y; e[2] = e4.z; e[3] = e4.w;
-                        }
+                            const float b[4] = {b4.x, b4.y, b4.z, b4.w};
+                            const int e[4] = {e4.x, e4.y, e4.z, e4.w};
 #pragma unroll
-                        for (int t = 0; t < 4; t++) f(c + t, (SCALED ? ldexpf(acc[i][j][4 * g + t], re + e[t]) : acc[i][j][4 * g + t]) + b[t]);
+                            for (int t = 0; t < 4; t++) f(c + t, ldexpf(acc[i][j][4 * g + t], re + e[t]) + b[t]);
+                        } else
+#pragma unroll
+                            for (int t = 0; t < 4; t++) f(c + t, acc[i][j][4 * g + t]);
                     }
             };
+            // (both walks read the accumulators where they are: the compiler would keep copies of 256 of them in between)
+            auto stay = [&] __attribute__((always_inline)) () {
+#pragma unroll
+                for (int j = 0; j < NB; j++) asm volatile("" : "+a"(acc[i][j]));
+            };
             float most = -INFINITY, sum[4] = {0.f, 0.f, 0.f, 0.f};
+            stay();
             outputs([&](int, float z) __attribute__((always_inline)) { most = fmaxf(most, z); });
             most = fmaxf(most, __shfl_xor(most, 32, 64));
             const float at = __builtin_isfinite(most) ? most : 0.f;
+            stay();
             outputs([&](int c, float z) __attribute__((always_inline)) { sum[c & 3] += exp_of(z - at); });
             float all = (sum[0] + sum[1]) + (sum[2] + sum[3]);
             all += __shfl_xor(all, 32, 64);
@@ -426,6 +474,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
             const int mine = label[wm0 + 32 * i + li] - wn0;
             if (__any(mine >= 0 && mine < 32 * NB)) {
                 float v = 0.f;
+                stay();
                 outputs([&](int c, float z) __attribute__((always_inline)) { v = mine - 4 * lh == c ? z : v; });
                 if (mine >= 0 && mine < 32 * NB && ((mine >> 2) & 1) == lh) p.target[m] = v;
             }
@@ -479,7 +528,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
             for (int r = 0; r < 32; r += RI) {
                 const int row = 32 * i + r + lane / QW;
                 const SmDzRow w = {lses[wm0 + row], weights[wm0 + row], label[wm0 + row], SCALED ? rexp[wm0 + row] : 0};
-                sm_dz<SCALED>(p, m0 + wm0 + row, c, get_row(r), w, k, sums);
+                sm_dz<SCALED, STARTED>(p, m0 + wm0 + row, c, get_row(r), w, k, sums);
             }
         }
         if (p.dbias) {
@@ -520,27 +569,27 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
                     const int row = 32 * i + r + lane / QW;
                     float v[4] = {u.x, u.y, u.z, u.w};
                     if (HOW != 0) sm_result<SCALED>(v, shift, factor[wm0 + row], p.alpha);
-                    if (VEC) {
-                        const unsigned at = c < p.N ? (unsigned)row * width + (unsigned)c * (HALF ? 2 : 4) : 0x80000000u;
-                        if (HOW == 2) {
-                            const float4 old = buffer_load4(rs, at);
-                            v[0] += p.beta * old.x; v[1] += p.beta * old.y; v[2] += p.beta * old.z; v[3] += p.beta * old.w;
-                        }
-                        if (ADD) {
-                            const float4 old = buffer_load4(as, c < p.N ? (unsigned)row * (unsigned)p.N * 4u + (unsigned)c * 4u : 0x80000000u);
-                            v[0] += old.x; v[1] += old.y; v[2] += old.z; v[3] += old.w;
-                        }
-                        if (HALF) {
-                            const owt_u32x2 o = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
-                            __builtin_amdgcn_raw_buffer_store_b64(o, rs, (int)at, 0, 0);
-                        } else {
-                            const owt_u32x4 o = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                            __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)at, 0, 0);
-                        }
-                    } else if (row < m_end) {
+                    // (rows that begin anywhere are written by fours, too, but for the last of them; memory takes them on any 4 bytes, and bf16 ones on any 2)
+                    const bool whole = VEC ? c < p.N : c + 4 <= p.N;
+                    const unsigned at = whole ? (unsigned)row * width + (unsigned)c * (HALF ? 2 : 4) : 0x80000000u;
+                    if (HOW == 2) {
+                        const float4 old = buffer_load4(rs, at);
+                        v[0] += p.beta * old.x; v[1] += p.beta * old.y; v[2] += p.beta * old.z; v[3] += p.beta * old.w;
+                    }
+                    if (ADD) {
+                        const float4 old = buffer_load4(as, whole ? (unsigned)row * (unsigned)p.N * 4u + (unsigned)c * 4u : 0x80000000u);
+                        v[0] += old.x; v[1] += old.y; v[2] += old.z; v[3] += old.w;
+                    }
+                    const owt_u32x2 h = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
+                    if (!HALF) {
+                        const owt_u32x4 o = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                        __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)at, 0, 0);
+                    } else if (VEC) __builtin_amdgcn_raw_buffer_store_b64(h, rs, (int)at, 0, 0);
+                    else if (whole && row < m_end) *(SmFourHalves *)(base + (size_t)row * width + 2 * c) = {h[0], h[1]};
+                    if (!VEC && !whole && row < m_end) {
                         char *w = base + (size_t)row * width;
 #pragma unroll
-                        for (int t = 0; t < 4; t++)
+                        for (int t = 0; t < 3; t++)
                             if (c + t < p.N) {
                                 if (HOW == 2) v[t] += p.beta * ((float *)w)[c + t];
                                 if (ADD) v[t] += add[(size_t)row * p.N + c + t];
