@@ -32,17 +32,23 @@ struct SmPrep {
     int x_rows;
 };
 
-// bf16 rows to whole steps, zeros behind them
+// 16 bytes from where rows begin anywhere
+struct __attribute__((packed, aligned(2))) SmLoose { uint32_t u[4]; };
+
+// bf16 rows to whole steps, zeros behind them: eight values a thread
 __global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep p)
 {
-    const size_t all = (size_t)p.out_rows * p.steps * 8, stride = (size_t)gridDim.x * 256;
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < all; i += stride) {
-        const int m = (int)(i / (unsigned)(p.steps * 8)), c = (int)(i % (unsigned)(p.steps * 8)) * 8;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (m < p.rows && c < p.cols && (!p.labels || has_class(p.labels[m], p.classes))) {
-            const uint16_t *row = (const uint16_t *)p.from + (size_t)m * p.cols;
-            if ((p.cols & 7) == 0) v = *(const uint4 *)(row + c);
-            else {
+    const int pieces = p.steps * 8;
+    for (int m = blockIdx.y; m < p.out_rows; m += gridDim.y) {
+        const bool real = m < p.rows && (!p.labels || has_class(p.labels[m], p.classes));
+        const uint16_t *row = (const uint16_t *)p.from + (size_t)m * p.cols;
+        for (int i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += gridDim.x * 256) {
+            const int c = 8 * i;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (real && c + 8 <= p.cols) {
+                const SmLoose l = *(const SmLoose *)(row + c);
+                v = make_uint4(l.u[0], l.u[1], l.u[2], l.u[3]);
+            } else if (real && c < p.cols) {
                 uint32_t u[4];
 #pragma unroll
                 for (int k = 0; k < 4; k++) {
@@ -51,8 +57,8 @@ __global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep p)
                 }
                 v = make_uint4(u[0], u[1], u[2], u[3]);
             }
+            *(uint4 *)(p.to + (size_t)m * pieces * 16 + 16 * i) = v;
         }
-        *(uint4 *)(p.to + i * 16) = v;
     }
 }
 
@@ -68,11 +74,13 @@ __device__ __forceinline__ int least_of_wave(int v)
     return v;
 }
 
-// fp32 rows as two f16 values under the power of two that brings a row's largest magnitude to [2^14, 2^15), one wavefront a row.  The row is read twice,
-// the second time from the caches.
-__global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
+// fp32 rows as two f16 values under the power of two that brings a row's largest magnitude to [2^14, 2^15), ROWS rows a work-group.  A row is read twice,
+// the second time from the caches.  Four rows a work-group for many rows, one for few (128 and 1000 rows of 4096: 9 and 14 us with four).
+template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, groups = (p.out_rows + 3) / 4;
+    constexpr int EACH = 256 / ROWS;        // threads of a row
+    __shared__ float part[4];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = threadIdx.x % EACH, groups = (p.out_rows + ROWS - 1) / ROWS;
     if ((int)blockIdx.x >= groups) {        // the least exponent of x's rows with their weights
         int least = kSmNone;
         for (int n = ((int)blockIdx.x - groups) * 256 + threadIdx.x; n < p.x_rows; n += ((int)gridDim.x - groups) * 256) {
@@ -86,44 +94,45 @@ __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
     }
     if (p.leasts && blockIdx.x == 0)        // x: before anything looks for them
         for (int i = threadIdx.x; i < p.leasts; i += 256) p.least[i] = kSmNone;
-    const int m = blockIdx.x * 4 + wave;
-    int exp = kSmNone;
-    if (m < p.out_rows) {
-        const bool real = m < p.rows && (!p.labels || has_class(p.labels[m], p.classes));
-        const float *row = (const float *)p.from + (size_t)m * p.cols;
-        const bool vec = (p.cols & 3) == 0;
-        auto four = [&](int c) __attribute__((always_inline)) {
-            if (!real || c >= p.cols) return make_float4(0.f, 0.f, 0.f, 0.f);
-            if (vec) return *(const float4 *)(row + c);
-            return make_float4(row[c], c + 1 < p.cols ? row[c + 1] : 0.f, c + 2 < p.cols ? row[c + 2] : 0.f, c + 3 < p.cols ? row[c + 3] : 0.f);
-        };
-        float most = 0.f;
-        if (real)
+    const int m = blockIdx.x * ROWS + threadIdx.x / EACH;
+    const bool real = m < p.rows && (!p.labels || has_class(p.labels[m], p.classes));
+    const float *row = (const float *)p.from + (size_t)m * p.cols;
+    auto four = [&](int c) __attribute__((always_inline)) {
+        if (!real || c >= p.cols) return make_float4(0.f, 0.f, 0.f, 0.f);
+        if (c + 4 <= p.cols) {
+            const SmLoose l = *(const SmLoose *)(row + c);
+            return make_float4(__uint_as_float(l.u[0]), __uint_as_float(l.u[1]), __uint_as_float(l.u[2]), __uint_as_float(l.u[3]));
+        }
+        return make_float4(row[c], c + 1 < p.cols ? row[c + 1] : 0.f, c + 2 < p.cols ? row[c + 2] : 0.f, 0.f);
+    };
+    float most = 0.f;
+    if (real)
 #pragma unroll 4
-            for (int c = 4 * lane; c < p.cols; c += 256) {
-                const float4 v = four(c);
-                most = fmaxf(fmaxf(fmaxf(most, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
-            }
+        for (int c = 4 * at; c < p.cols; c += 4 * EACH) {
+            const float4 v = four(c);
+            most = fmaxf(fmaxf(fmaxf(most, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
+        }
 #pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
-        // (a row of infinities stays as it is: they are infinite in f16, too)
-        if (most > 0.f) exp = __builtin_isfinite(most) ? kSmTop - ilogbf(most) : 0;
-        const int shift = exp == kSmNone ? 0 : exp;     // (NaN alone has no largest magnitude, and stays NaN)
+    for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
+    if (ROWS == 1) {
+        if (lane == 0) part[wave] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        __syncthreads();
+    }
+    // (a row of infinities stays as it is: they are infinite in f16, too; NaN alone has no largest magnitude, and stays NaN)
+    const int exp = !(most > 0.f) ? kSmNone : __builtin_isfinite(most) ? kSmTop - ilogbf(most) : 0, shift = exp == kSmNone ? 0 : exp;
+    if (m < p.out_rows) {
         unsigned char *to = p.to + (size_t)m * p.steps * 256;
 #pragma unroll 4
-        for (int c = 4 * lane; c < p.steps * 64; c += 256) {
+        for (int c = 4 * at; c < p.steps * 64; c += 4 * EACH) {
             const float4 v = four(c);
             const float s[4] = {ldexpf(v.x, shift), ldexpf(v.y, shift), ldexpf(v.z, shift), ldexpf(v.w, shift)};
             sm_put_halves(to + (size_t)(c >> 6) * 256 + 2 * (c & 63), s);
         }
-        if (lane == 0 && m < p.rows) p.exps[m] = exp;
+        if (at == 0 && m < p.rows) p.exps[m] = exp;
     }
-    if (p.piece >= 0) {
-        __shared__ int part[4];
-        if (lane == 0) part[wave] = exp;
-        __syncthreads();
-        if (threadIdx.x == 0) lower(p.least + 1 + p.piece, min(min(part[0], part[1]), min(part[2], part[3])));
-    }
+    if (p.piece >= 0 && at == 0 && m < p.rows) lower(p.least + 1 + p.piece, exp);
 }
 
 // ------------------------------------------------------------------------------------------------ after the products
@@ -349,34 +358,36 @@ static owt_status need_ws(const void *ws, size_t have, size_t need)
     return OWT_OK;
 }
 
-// What a work-group takes: `start` for its beginning and end, `step` for a step on a quiet chip, `busy` where 128 or more run (256 x 256: all 256).
-struct SmTileCost { int bm, bn, wm, wn; float start, step, busy; };
-static const SmTileCost kSmTiles[SM_TILES] = {{256, 256, 2, 2, 11.f, 1.05f, 1.5f}, {128, 128, 2, 2, 3.f, 0.4f, 0.55f}, {64, 64, 2, 2, 1.2f, 0.21f, 0.21f},
-                                              {32, 256, 1, 4, 2.f, 0.3f, 1.0f}};
+// What a work-group takes: `start` for its beginning and end (`dz` more where outputs leave as dz), `step` for a step on a quiet chip, `busy` where most CUs have one.
+// us, fitted to outputs, dz, dx and dw of 16 x 2048 -> 65536, 128 x 4096 -> 32768, 777 x 1536 -> 20000, 2048 x 2048 -> 16384 (bf16) and 1003 x 1024 -> 16384 (fp32)
+// with every tile.  Two work-groups a CU take turns, so that what counts is how many there are, not how many rounds.
+struct SmTileCost { int bm, bn, wm, wn; float start, dz, step, busy; int together; };
+static const SmTileCost kSmTiles[SM_TILES] = {{256, 256, 2, 2, 11.f, 8.f, 1.05f, 1.5f, 1}, {128, 128, 2, 2, 3.f, 2.f, 0.4f, 0.55f, 1},
+                                              {128, 128, 2, 2, 2.f, 1.5f, 0.6f, 0.5f, 2}, {64, 64, 2, 2, 1.2f, 0.5f, 0.21f, 0.21f, 1}};
 constexpr int SM_NOTHING = -1;          // more work-groups than a launch holds
 struct SmPlan { int tile, splits; float us; };
 static int up(int n, int to) { return (n + to - 1) / to; }
 
-// `outputs`: sums that are split cost a pass over N x cols of them; results of dx and dw do, too
-static SmPlan sm_plan(long M, long N, int steps, bool few)
+// A product of M x N results and `steps` steps, `products` of which stay together; dz: they leave as dz
+static SmPlan sm_plan(long M, long N, int steps, int products, bool dz)
 {
     SmPlan best{SM_NOTHING, 1, 1e30f};
-    const int want = forced_tile() - kSmFirstTile, want_split = forced_split();
+    const int want = forced_tile() - kSmFirstTile, want_split = forced_split(), most = steps / products;
     for (int t = 0; t < SM_TILES; t++) {
-        if (t == SM_FEW && !few) continue;
-        if (want >= 0 && want < SM_TILES && t != want && (want != SM_FEW || few)) continue;
+        if (want >= 0 && want < SM_TILES && t != want) continue;
         const SmTileCost &q = kSmTiles[t];
         const long tiles = ((M + q.bm - 1) / q.bm) * ((N + q.bn - 1) / q.bn);
         if (!groups_fit(tiles, 256)) continue;
-        for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= steps && tiles * sp <= 1024)); sp *= 2) {
-            const long each = (tiles * sp + 255) / 256;         // work-groups of a CU
-            const float step = tiles * sp >= (t == SM_BIG ? 256 : 128) ? q.busy : q.step;
-            float us = 3.f + (float)each * (q.start + (float)up(steps, sp) * step);
+        for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= most && tiles * sp <= 1024)); sp *= 2) {
+            const long n = tiles * sp;
+            const float step = n >= (t == SM_BIG ? 192 : 128) ? q.busy : q.step, one = q.start + (dz && sp == 1 ? q.dz : 0.f) + (float)(up(most, sp) * products) * step;
+            const float each = q.together > 1 && n > 256 ? (float)n / 256.f + 0.5f : (float)((n + 255) / 256);      // work-groups of a CU
+            float us = 3.f + each * (q.together > 1 && n <= 256 ? q.start + (one - q.start) * 1.2f : one);
             if (sp > 1) us += 3.6f + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
             if (us < best.us) best = {t, sp, us};
         }
     }
-    if (want_split > 0) best.splits = want_split < steps ? want_split : steps;
+    if (want_split > 0) best.splits = want_split < most ? want_split : most;
     return best;
 }
 static size_t partial_bytes(const SmPlan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
@@ -397,9 +408,9 @@ struct SmLayout {
         laid = half || I % 64;
         products = half ? SM_THREE : SM_ONE;
         const size_t row = (size_t)isteps * (half ? 256 : 128);
-        piece = forward ? forward_piece(row, ol) : backward_piece(N, row, ol);
+        piece = forward ? forward_piece(laid, row, ol) : backward_piece(laid, half, N, row, ol);
         pieces = ol ? up(ol, piece) : 0;
-        z = sm_plan(N, piece, isteps * products, true);
+        z = sm_plan(N, piece, isteps * products, products, !forward);
         if (forward && pieces > 1) z.splits = 1;        // (a split row's outputs are joined in one go)
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
@@ -418,8 +429,8 @@ struct SmLayout {
             label_out = take((size_t)N * 4);
         } else {
             const int psteps = up(piece, 64);
-            dx = sm_plan(N, I, psteps * (half ? SM_THREE : SM_ONE), true);
-            dw = sm_plan(piece, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), false);
+            dx = sm_plan(N, I, psteps * (half ? SM_THREE : SM_ONE), half ? SM_THREE : SM_ONE, false);
+            dw = sm_plan(piece, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), half ? SM_THREE : SM_PAIR, false);
             dz = take((size_t)N * psteps * 256);
             dz_dx = take(half ? (size_t)N * psteps * 256 : 0);
             dxs = take(!half && pieces > 1 ? (size_t)N * I * 4 : 0);
@@ -432,19 +443,21 @@ struct SmLayout {
         total = N ? at : 0;
     }
     bool fits() const { return z.tile >= 0 && dx.tile >= 0 && dw.tile >= 0; }
-    // Weights that are laid out go in pieces of at most 128 MB; outputs are not kept, so that the others are one piece.
-    int forward_piece(size_t row, int ol) const
+    // Classes of a piece: as many as `fit`, but pieces alike
+    static int alike(size_t fit, size_t least, int ol)
     {
-        if (!laid) return ol;
-        const size_t fit = ((size_t)128 << 20) / row / 256 * 256;
-        return fit < 256 ? (ol < 256 ? ol : 256) : fit < (size_t)ol ? (int)fit : ol;
+        fit = fit < least ? least : fit;
+        if (fit >= (size_t)ol) return ol;
+        const int pieces = (int)((ol + fit - 1) / fit);
+        return up(up(ol, pieces), 256) * 256;
     }
-    int backward_piece(int N, size_t row, int ol) const
+    // Weights that are laid out go in pieces of at most 256 MB; outputs are not kept, so that the others are one piece.
+    static int forward_piece(bool laid, size_t row, int ol) { return laid ? alike(((size_t)256 << 20) / row, 256, ol) : ol; }
+    // dz, and weights that are laid out, stay in the 256 MB behind the L2 caches between the product that writes them and those that read them
+    static int backward_piece(bool laid, bool half, int N, size_t row, int ol)
     {
         const size_t each = (size_t)N * (half ? 8 : 4) + (laid ? row : 0);
-        size_t fit = ((size_t)128 << 20) / (each ? each : 1) / 256 * 256;
-        fit = fit < 1024 ? 1024 : fit;
-        return fit < (size_t)ol ? (int)fit : ol;
+        return alike(((size_t)128 << 20) / (each ? each : 1), 1024, ol);
     }
 };
 
@@ -513,8 +526,9 @@ struct SmSource {
         if (l.half) {
             p.least = (int *)(ws + l.least);
             const unsigned more = p.x_exps ? groups_of(p.x_rows, 64) : 0;
-            hipLaunchKernelGGL(sm_halves_kernel, dim3((unsigned)up(p.out_rows, 4) + more), dim3(256), 0, s, p);
-        } else hipLaunchKernelGGL(sm_rows_kernel, dim3(groups_of((size_t)p.out_rows * p.steps * 8, 8192)), dim3(256), 0, s, p);
+            if (p.out_rows >= 4096) hipLaunchKernelGGL(sm_halves_kernel<4>, dim3((unsigned)up(p.out_rows, 4) + more), dim3(256), 0, s, p);
+            else hipLaunchKernelGGL(sm_halves_kernel<1>, dim3((unsigned)p.out_rows + more), dim3(256), 0, s, p);
+        } else hipLaunchKernelGGL(sm_rows_kernel, dim3((unsigned)up(p.steps * 8, 256), (unsigned)(p.out_rows < 32768 ? p.out_rows : 32768)), dim3(256), 0, s, p);
     }
     // backward: rows without a class and those up to a whole step are zeros
     SmOperand x(const void *from, const int *labels, bool forward) const
@@ -684,6 +698,7 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
         q.least = least;
         q.partial = p.partial;
         q.out = dw + (size_t)v0 * d->I;
+        q.big = (size_t)ol * d->I * 4 > (32u << 20);
         if ((e = results(l.half, SM_PRODUCT_DW, q, l.dw, s)) != hipSuccess) return launched(e);
     }
     return launched();

@@ -91,6 +91,7 @@ struct SmParams {
     // results
     void *out;              // C, rows of N values
     int bf16;               // its type
+    int big;                // it is more than an eighth of the 256 MB behind the L2 caches
     float alpha, beta;      // beta only where results are fp32
     const float *add;       // fp32 [M][N] that is added to alpha times the sum (may be out), or null
     const int *least;       // (f16 values) results are the sums times 2^-(*least + kSmDzTop)
@@ -555,8 +556,9 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
         const int m_end = __builtin_amdgcn_readfirstlane(max(0, min(32 * MB, p.M - m0 - wm0)));     // rows of this wavefront that exist
         const float *add = p.add ? p.add + (size_t)(m0 + wm0) * p.N : nullptr;
         auto ends = [&](auto how, auto vec) __attribute__((always_inline)) {
-            constexpr int HOW = decltype(how)::value;       // 0: parts, 1: fp32, 2: fp32 with beta, 3: bf16; 4 on: something is added
-            constexpr bool VEC = decltype(vec)::value, HALF = HOW == 3 || HOW == 5, ADD = HOW >= 4;
+            constexpr int HOW = decltype(how)::value;       // 0: parts, 1: fp32, 2: fp32 with beta, 3: bf16; 4, 5: something is added; 6: fp32, past the caches
+            constexpr bool VEC = decltype(vec)::value, HALF = HOW == 3 || HOW == 5, ADD = HOW == 4 || HOW == 5;
+            constexpr int PAST = HOW == 6 ? 2 : 0;
             // whole fours: through a descriptor that ends with the last row, where what lies outside is not written
             const __amdgpu_buffer_rsrc_t rs = owt_make_rsrc(sm_uniform((const unsigned char *)base), (unsigned)m_end * width);
             const __amdgpu_buffer_rsrc_t as = owt_make_rsrc(sm_uniform((const unsigned char *)add), ADD ? (unsigned)m_end * (unsigned)p.N * 4u : 0u);
@@ -583,7 +585,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
                     const owt_u32x2 h = {f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3])};
                     if (!HALF) {
                         const owt_u32x4 o = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-                        __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)at, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(o, rs, (int)at, 0, PAST);
                     } else if (VEC) __builtin_amdgcn_raw_buffer_store_b64(h, rs, (int)at, 0, 0);
                     else if (whole && row < m_end) *(SmFourHalves *)(base + (size_t)row * width + 2 * c) = {h[0], h[1]};
                     if (!VEC && !whole && row < m_end) {
@@ -608,6 +610,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
                 else ends(integral_constant<int, 4>{}, vec);
             } else if (p.bf16) ends(integral_constant<int, 3>{}, vec);
             else if (p.beta != 0.f) ends(integral_constant<int, 2>{}, vec);
+            else if (p.big) ends(integral_constant<int, 6>{}, vec);
             else ends(integral_constant<int, 1>{}, vec);
         };
         if ((p.N & 3) == 0) with(std::true_type{});

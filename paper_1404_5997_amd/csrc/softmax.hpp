@@ -5,12 +5,14 @@
 
 namespace owt {
 
-// 256 x 256, 128 x 128, 64 x 64, and 32 x 256 for few rows (not of dw, whose rows are classes).  owt_test_force_variant: 120.. name these.
+// 256 x 256; 128 x 128 with three stages, one work-group a CU, and with two stages, two a CU; 64 x 64.  owt_test_force_variant: 120.. name these.
+// The pair of 128 x 128 covers one another's beginnings and ends where there are enough of them, the single one has more on its way where there are few (us, one and the
+// other: outputs of 777 rows 1536 -> 20000, 1104 tiles, 86 and 69, their dx, 88 tiles, 161 and 210).  256 x 128 and 32 x 256 were never the fastest.
 typedef SmShape<2, 2, 4, 4, 2, 1> SmBig;
 typedef SmShape<2, 2, 2, 2, 3, 1> SmMid;
+typedef SmShape<2, 2, 2, 2, 2, 2> SmPair;
 typedef SmShape<2, 2, 1, 1, 4, 2> SmSmall;
-typedef SmShape<1, 4, 1, 2, 4, 1> SmFew;
-enum { SM_BIG, SM_MID, SM_SMALL, SM_FEW, SM_TILES };
+enum { SM_BIG, SM_MID, SM_TWO, SM_SMALL, SM_TILES };
 constexpr int kSmFirstTile = 120;
 
 enum { SM_PRODUCT_TOP, SM_PRODUCT_DZ, SM_PRODUCT_Z, SM_PRODUCT_DX, SM_PRODUCT_DW };

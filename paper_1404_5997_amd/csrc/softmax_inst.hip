@@ -18,8 +18,8 @@ template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmP
 {
     if (tile == SM_BIG) return go<TA, TB, SmBig, END>(p, s);
     if (tile == SM_MID) return go<TA, TB, SmMid, END>(p, s);
+    if (tile == SM_TWO) return go<TA, TB, SmPair, END>(p, s);
     if (tile == SM_SMALL) return go<TA, TB, SmSmall, END>(p, s);
-    if constexpr (!TA) return go<TA, TB, SmFew, END>(p, s);
     return hipErrorInvalidValue;
 }
 

@@ -320,7 +320,7 @@ def test_two_calls_at_once_on_streams_of_their_own():
 
 # ------------------------------------------------------------------------------------------------ every tile, and sums that are split
 
-TILES = {"256x256": 120, "128x128": 121, "64x64": 122, "32x256": 123}
+TILES = {"256x256": 120, "128x128": 121, "128x128, two a CU": 122, "64x64": 123}
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
