@@ -17,84 +17,25 @@ namespace owt {
 
 // ------------------------------------------------------------------------------------------------ layout of operands
 
-struct SmPrep {
-    const void *from;           // [rows][cols]
-    unsigned char *to;          // rows of `steps` steps
-    int rows, out_rows, cols, steps;
-    const int *labels;          // rows without a class become zeros (null: none do)
-    int classes;
-    const float *weight;        // of the rows, or null
-    int *exps;                  // fp32: of each row
-    // fp32: [0] takes the least of x's exponents less those of the weights, [1 + piece] those of w's pieces.  Laying out x sets all of them; the first
-    // piece's w finds the first, from x's exponents (x_rows of them) by work-groups of its own.
-    int *least, leasts, piece;
-    const int *x_exps;
-    int x_rows;
-};
-
-// 16 bytes from where rows begin anywhere
-struct __attribute__((packed, aligned(2))) SmLoose { uint32_t u[4]; };
-
-// bf16 rows to whole steps, zeros behind them: eight values a thread
-__global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep p)
+// Rows of x (a) and of w (b), either of which may be none, in one launch.
+__global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep a, const SmPrep b, int groups_a)
 {
-    const int pieces = p.steps * 8;
-    for (int m = blockIdx.y; m < p.out_rows; m += gridDim.y) {
-        const bool real = m < p.rows && (!p.labels || has_class(p.labels[m], p.classes));
-        const uint16_t *row = (const uint16_t *)p.from + (size_t)m * p.cols;
-        for (int i = blockIdx.x * 256 + threadIdx.x; i < pieces; i += gridDim.x * 256) {
-            const int c = 8 * i;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (real && c + 8 <= p.cols) {
-                const SmLoose l = *(const SmLoose *)(row + c);
-                v = make_uint4(l.u[0], l.u[1], l.u[2], l.u[3]);
-            } else if (real && c < p.cols) {
-                uint32_t u[4];
-#pragma unroll
-                for (int k = 0; k < 4; k++) {
-                    const int a = c + 2 * k;
-                    u[k] = (a < p.cols ? row[a] : 0u) | ((a + 1 < p.cols ? (uint32_t)row[a + 1] : 0u) << 16);
-                }
-                v = make_uint4(u[0], u[1], u[2], u[3]);
-            }
-            *(uint4 *)(p.to + (size_t)m * pieces * 16 + 16 * i) = v;
-        }
-    }
-}
-
-// Every work-group has a word to say, and hardly any a new one: the others only look (4096 atomics on one word took 50 us).
-__device__ __forceinline__ void lower(int *least, int v)
-{
-    if (v < __hip_atomic_load(least, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)) atomicMin(least, v);
-}
-__device__ __forceinline__ int least_of_wave(int v)
-{
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) v = min(v, __shfl_xor(v, d, 64));
-    return v;
+    if ((int)blockIdx.x < groups_a) sm_copy_rows(a, blockIdx.x, groups_a);
+    else sm_copy_rows(b, blockIdx.x - groups_a, gridDim.x - groups_a);
 }
 
 // fp32 rows as two f16 values under the power of two that brings a row's largest magnitude to [2^14, 2^15), ROWS rows a work-group.  A row is read twice,
-// the second time from the caches.  Four rows a work-group for many rows, one for few (128 and 1000 rows of 4096: 9 and 14 us with four).
-template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep p)
+// the second time from the caches.  Four rows a work-group for many rows, one for few.
+template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep a, const SmPrep b, int groups_a)
 {
     constexpr int EACH = 256 / ROWS;        // threads of a row
     __shared__ float part[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = threadIdx.x % EACH, groups = (p.out_rows + ROWS - 1) / ROWS;
-    if ((int)blockIdx.x >= groups) {        // the least exponent of x's rows with their weights
-        int least = kSmNone;
-        for (int n = ((int)blockIdx.x - groups) * 256 + threadIdx.x; n < p.x_rows; n += ((int)gridDim.x - groups) * 256) {
-            const float g = p.weight ? fabsf(p.weight[n]) : 1.f;
-            // a weight is below 2^k (one that is zero or not finite says nothing)
-            if (p.x_exps[n] != kSmNone && g > 0.f && __builtin_isfinite(g)) least = min(least, p.x_exps[n] - (ilogbf(g) + 1));
-        }
-        least = least_of_wave(least);
-        if (lane == 0) lower(p.least, least);
-        return;
-    }
-    if (p.leasts && blockIdx.x == 0)        // x: before anything looks for them
-        for (int i = threadIdx.x; i < p.leasts; i += 256) p.least[i] = kSmNone;
-    const int m = blockIdx.x * ROWS + threadIdx.x / EACH;
+    __shared__ int low[4];
+    const bool of_a = (int)blockIdx.x < groups_a;
+    const SmPrep &p = of_a ? a : b;
+    const int group = of_a ? blockIdx.x : blockIdx.x - groups_a;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = threadIdx.x % EACH;
+    const int m = group * ROWS + threadIdx.x / EACH;
     const bool real = m < p.rows && (!p.labels || has_class(p.labels[m], p.classes));
     const float *row = (const float *)p.from + (size_t)m * p.cols;
     auto four = [&](int c) __attribute__((always_inline)) {
@@ -118,7 +59,6 @@ template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(cons
         if (lane == 0) part[wave] = most;
         __syncthreads();
         most = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-        __syncthreads();
     }
     // (a row of infinities stays as it is: they are infinite in f16, too; NaN alone has no largest magnitude, and stays NaN)
     const int exp = !(most > 0.f) ? kSmNone : __builtin_isfinite(most) ? kSmTop - ilogbf(most) : 0, shift = exp == kSmNone ? 0 : exp;
@@ -132,7 +72,15 @@ template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(cons
         }
         if (at == 0 && m < p.rows) p.exps[m] = exp;
     }
-    if (p.piece >= 0 && at == 0 && m < p.rows) lower(p.least + 1 + p.piece, exp);
+    if (!p.lows) return;                    // (of all threads, or of none)
+    // a weight is below 2^k (a row whose weight is zero or not finite says nothing)
+    const float g = p.weight && m < p.rows ? fabsf(p.weight[m]) : 1.f;
+    const int mine = m < p.rows && exp != kSmNone && g > 0.f && __builtin_isfinite(g) ? exp - (p.weight ? ilogbf(g) + 1 : 0) : kSmNone;
+    if (ROWS > 1) {
+        if (lane == 0) low[wave] = mine;
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) p.lows[group] = ROWS == 1 ? mine : min(min(low[0], low[1]), min(low[2], low[3]));
 }
 
 // ------------------------------------------------------------------------------------------------ after the products
@@ -211,6 +159,8 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_top_kerne
 template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_dz_kernel(const SmParams p)
 {
     __shared__ float4 part[16][16];
+    __shared__ int two[8];
+    const int2 least = SCALED ? sm_leasts(p, two, blockIdx.x == 0 && blockIdx.y == 0) : make_int2(0, 0);
     const int q = threadIdx.x & 15, r = threadIdx.x >> 4, c = blockIdx.x * 64 + 4 * q;
     const size_t whole = (size_t)p.M * p.N;
     const SmDzColumns k = sm_dz_columns<SCALED>(p, c);
@@ -230,7 +180,7 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_dz_kernel
 #pragma unroll
                 for (int t = 0; t < 4; t++)
                     if (c + t < p.N && m < p.M) z[t] += row[s * whole + t];
-        sm_dz<SCALED, false>(p, m, c, make_float4(z[0], z[1], z[2], z[3]), sm_dz_row<SCALED>(p, m), k, sums);
+        sm_dz<SCALED, false>(p, least, m, c, make_float4(z[0], z[1], z[2], z[3]), sm_dz_row<SCALED>(p, m), k, sums);
     }
     if (!p.dbias) return;
     part[r][q] = make_float4(sums[0], sums[1], sums[2], sums[3]);
@@ -247,7 +197,7 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_join_kernel(con
 {
     const unsigned quads = (unsigned)(p.N + 3) / 4;
     const size_t n = (size_t)p.M * quads, stride = (size_t)gridDim.x * 256, whole = (size_t)p.M * p.N;
-    const int shift = SCALED && p.splits ? -(*p.least + kSmDzTop) : 0;
+    const int shift = SCALED && p.splits ? -(*p.under + kSmDzTop) : 0;
     const bool vec = (p.N & 3) == 0;
     for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += stride) {
         const int m = (int)(i / quads), c = (int)(i % quads) * 4;
@@ -290,17 +240,6 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_join_kernel(con
                     else store1((float *)p.out, at + t, v[t]);
                 }
     }
-}
-
-// dbias from the sums over strips of rows
-__global__ void __launch_bounds__(256) sm_dbias_kernel(const float *sums, int strips, int cols, float alpha, float beta, float *db)
-{
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c >= cols) return;
-    float s = 0.f;
-#pragma unroll 8
-    for (int k = 0; k < strips; k++) s += sums[(size_t)k * cols + c];
-    db[c] = alpha * s + (beta != 0.f ? beta * db[c] : 0.f);
 }
 
 // Joins the shards' shares: lse and target of `workers` shards, worker by worker.
@@ -393,13 +332,44 @@ static SmPlan sm_plan(long M, long N, int steps, int products, bool dz)
 static size_t partial_bytes(const SmPlan &pl, long M, long N) { return pl.splits > 1 ? (size_t)pl.splits * M * N * 4 : 0; }
 static int strips_of(const SmPlan &z, int N) { return z.splits > 1 ? up(N, 32) : up(N, kSmTiles[z.tile].bm) * kSmTiles[z.tile].wm; }
 
+// Both backward products in one launch, dx's sums perhaps split: worth its tile where neither fills the chip for long.  Returns the tile or SM_NOTHING, the plan of dx in x.
+static int sm_pair(long N, long cols, long I, bool half, const SmPlan &dx, const SmPlan &dw, SmPlan &x)
+{
+    const int want = forced_tile() - kSmFirstTile, products_x = half ? SM_THREE : SM_ONE, products_w = half ? SM_THREE : SM_PAIR;
+    const int most = up((int)cols, 64), steps_w = up((int)N, 64) * products_w;
+    if (forced_split() > 0) return SM_NOTHING;
+    float least = want >= 0 && want < SM_TILES ? 1e30f : dx.us + dw.us;
+    int best = SM_NOTHING;
+    for (int t : {(int)SM_MID, (int)SM_SMALL}) {
+        if (want >= 0 && want < SM_TILES && t != want) continue;
+        const SmTileCost &q = kSmTiles[t];
+        const long nx = ((N + q.bm - 1) / q.bm) * ((I + q.bn - 1) / q.bn), nw = ((cols + q.bm - 1) / q.bm) * ((I + q.bn - 1) / q.bn);
+        if (!groups_fit(nx * 32 + nw + 16, 256)) continue;
+        for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= most && nx * sp <= 1024)); sp *= 2) {
+            const float ux = q.start + (float)(up(most, sp) * products_x) * q.busy, uw = q.start + (float)steps_w * q.busy, longest = ux > uw ? ux : uw;
+            const float sum = ((float)(nx * sp) * ux + (float)nw * uw) / 256.f + 0.3f * longest;
+            float us = 3.f + (sum > longest ? sum : longest);
+            if (sp > 1) us += 3.6f + (float)(sp + 1) * (float)N * (float)I * 4.f / 3e6f;
+            if (us < least) {
+                least = us;
+                best = t;
+                x = {t, sp, us};
+            }
+        }
+    }
+    return best;
+}
+static int low_groups(size_t rows) { return rows >= 4096 ? (int)((rows + 3) / 4) : (int)rows; }
+
 // Scratch of a pass, laid out in order.
 struct SmLayout {
     bool half, laid;            // fp32; w is laid out
     int isteps, piece, pieces;  // steps of memory of a row of x or w; classes of a piece, pieces
     int products;               // of outputs and of dx, per step of memory
     SmPlan z, dx, dw;           // of a whole piece
-    size_t x, w, xexp, wexp, least, top, label_out, dz, dz_dx, dxs, strips, partial, total;
+    int pair;                   // the tile of dx and dw in one launch, or nothing
+    SmPlan together;            // dx's part of it
+    size_t x, w, xexp, wexp, xlows, wlows, least, top, label_out, dz, dz_dx, dxs, strips, partial, total;
     SmLayout(const owt_fc_desc *d, int ol, bool forward)
     {
         const int N = d->N, I = d->I;
@@ -419,7 +389,10 @@ struct SmLayout {
         w = take(laid ? (size_t)piece * row : 0);
         xexp = take(half ? (size_t)N * 4 : 0);
         wexp = take(half ? (size_t)piece * 4 : 0);
-        least = take(half ? (size_t)(pieces + 1) * 4 : 0);
+        xlows = take(half && !forward ? (size_t)low_groups(rows) * 4 : 0);
+        wlows = take(half && !forward ? (size_t)low_groups(piece) * 4 : 0);
+        least = take(half && !forward ? 8 : 0);
+        pair = SM_NOTHING;
         top = label_out = dz = dz_dx = dxs = strips = partial = total = 0;
         dx = dw = z;
         if (z.tile < 0) return;
@@ -435,6 +408,11 @@ struct SmLayout {
             dz_dx = take(half ? (size_t)N * psteps * 256 : 0);
             dxs = take(!half && pieces > 1 ? (size_t)N * I * 4 : 0);
             strips = take((size_t)strips_of(z, N) * piece * 4);
+            pair = sm_pair(N, piece, I, half, dx, dw, together);
+            if (pair != SM_NOTHING) {
+                dx = together;
+                dw = {pair, 1, 0.f};
+            }
             const size_t a = partial_bytes(dx, N, I), b = partial_bytes(dw, piece, I);
             parts = parts > a ? parts : a;
             parts = parts > b ? parts : b;
@@ -519,53 +497,67 @@ struct SmSource {
     {
         return {o.at, o.ld, 64 * o.ld, rows, 8 * steps, o.planes};
     }
-    void lay(SmPrep p) const
+    // x for the products: backward, rows without a class and those up to a whole step are zeros
+    SmPrep x_rows(const void *from, const int *labels, const float *weight, bool forward) const
     {
-        p.cols = d->I;
-        p.steps = l.isteps;
-        if (l.half) {
-            p.least = (int *)(ws + l.least);
-            const unsigned more = p.x_exps ? groups_of(p.x_rows, 64) : 0;
-            if (p.out_rows >= 4096) hipLaunchKernelGGL(sm_halves_kernel<4>, dim3((unsigned)up(p.out_rows, 4) + more), dim3(256), 0, s, p);
-            else hipLaunchKernelGGL(sm_halves_kernel<1>, dim3((unsigned)p.out_rows + more), dim3(256), 0, s, p);
-        } else hipLaunchKernelGGL(sm_rows_kernel, dim3((unsigned)up(p.steps * 8, 256), (unsigned)(p.out_rows < 32768 ? p.out_rows : 32768)), dim3(256), 0, s, p);
-    }
-    // backward: rows without a class and those up to a whole step are zeros
-    SmOperand x(const void *from, const int *labels, bool forward) const
-    {
-        if (forward && !l.laid) return along(from, d->N);
         SmPrep p;
         memset(&p, 0, sizeof(p));
         p.from = from;
         p.to = (unsigned char *)(ws + l.x);
         p.rows = d->N;
         p.out_rows = forward ? d->N : up(d->N, 64) * 64;
+        p.cols = d->I;
+        p.steps = l.isteps;
         p.labels = forward ? nullptr : labels;
         p.classes = d->O_total;
+        p.weight = weight;
         p.exps = (int *)(ws + l.xexp);
-        p.leasts = l.pieces + 1;
-        p.piece = -1;
-        lay(p);
-        return along(ws + l.x, d->N);
+        p.lows = forward ? nullptr : (int *)(ws + l.xlows);
+        return p;
     }
-    SmOperand w(const void *from, int piece, int v0, int cols, const float *weight, bool forward) const
+    SmPrep w_rows(const void *from, int v0, int cols, bool forward) const
     {
-        const char *at = (const char *)from + (size_t)v0 * d->I * (l.half ? 4 : 2);
-        if (!l.laid) return along(at, cols);
         SmPrep p;
         memset(&p, 0, sizeof(p));
-        p.from = at;
+        p.from = (const char *)from + (size_t)v0 * d->I * (l.half ? 4 : 2);
         p.to = (unsigned char *)(ws + l.w);
         p.rows = p.out_rows = cols;
+        p.cols = d->I;
+        p.steps = l.isteps;
         p.exps = (int *)(ws + l.wexp);
-        p.piece = piece;
-        if (!forward && piece == 0) {
-            p.weight = weight;
-            p.x_exps = (const int *)(ws + l.xexp);
-            p.x_rows = d->N;
+        p.lows = forward ? nullptr : (int *)(ws + l.wlows);
+        return p;
+    }
+    void lay(const SmPrep &a, const SmPrep &b) const
+    {
+        if (l.half) {
+            // (x's and w's work-groups are of one kind where both are few or both are many; else each has a launch)
+            const bool many_a = a.out_rows >= 4096, many_b = b.out_rows >= 4096;
+            if (a.out_rows && b.out_rows && many_a != many_b) {
+                SmPrep none;
+                memset(&none, 0, sizeof(none));
+                lay(a, none);
+                lay(none, b);
+                return;
+            }
+            const int ga = low_groups(a.out_rows), gb = low_groups(b.out_rows);
+            if (many_a || many_b) hipLaunchKernelGGL(sm_halves_kernel<4>, dim3((unsigned)(ga + gb)), dim3(256), 0, s, a, b, ga);
+            else hipLaunchKernelGGL(sm_halves_kernel<1>, dim3((unsigned)(ga + gb)), dim3(256), 0, s, a, b, ga);
+        } else {
+            auto groups = [&](const SmPrep &p) { const long n = (long)p.out_rows * up(p.steps * 8, 256); return (int)(n < 8192 ? n : 8192); };
+            hipLaunchKernelGGL(sm_rows_kernel, dim3((unsigned)(groups(a) + groups(b))), dim3(256), 0, s, a, b, groups(a));
         }
-        lay(p);
-        return along(ws + l.w, cols);
+    }
+    // operands of a piece's outputs; x is laid out with the first
+    void operands(const void *x, const void *w, int piece, int v0, int cols, const int *labels, const float *weight, bool forward, SmOperand &xo, SmOperand &wo) const
+    {
+        if (l.laid) {
+            SmPrep a = x_rows(x, labels, weight, forward);
+            if (piece) a.out_rows = 0;
+            lay(a, w_rows(w, v0, cols, forward));
+        }
+        xo = along(l.laid ? ws + l.x : x, d->N);
+        wo = along(l.laid ? ws + l.w : (const char *)w + (size_t)v0 * d->I * 2, cols);
     }
 };
 
@@ -597,11 +589,11 @@ static owt_status forward(const owt_fc_desc *d, const SmLayout &l, int ol, const
                           float *loss, char *ws, hipStream_t s)
 {
     const SmSource from{d, l, ws, s};
-    const SmOperand xo = from.x(x, nullptr, true);
     SmRows r = {(const Top *)(ws + l.top), 0, d->N, (const float *)(ws + l.label_out), labels, d->O_total, d->rank * ol, ol, lse, target, loss};
     for (int k = 0; k < l.pieces; k++) {
         const int v0 = k * l.piece, cols = ol - v0 < l.piece ? ol - v0 : l.piece;
-        const SmOperand wo = from.w(w, k, v0, cols, nullptr, true);
+        SmOperand xo, wo;
+        from.operands(x, w, k, v0, cols, nullptr, nullptr, true, xo, wo);
         SmParams p = outputs(d, l, ws, xo, wo, ol, v0, cols, bias, labels);
         p.target = (float *)(ws + l.label_out);
         p.top = (Top *)(ws + l.top) + (size_t)r.parts * d->N;
@@ -641,21 +633,25 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
         return launched();
     }
     const SmSource from{d, l, ws, s};
-    const SmOperand xo = from.x(x, labels, false);
     const int products = l.half ? SM_THREE : SM_PAIR, nsteps = up(d->N, 64);
     int *least = (int *)(ws + l.least);
     for (int k = 0; k < l.pieces; k++) {
         const int v0 = k * l.piece, cols = ol - v0 < l.piece ? ol - v0 : l.piece, psteps = up(cols, 64);
-        const SmOperand wo = from.w(w, k, v0, cols, weight, false);
+        SmOperand xo, wo;
+        from.operands(x, w, k, v0, cols, labels, weight, false, xo, wo);
         SmParams p = outputs(d, l, ws, xo, wo, ol, v0, cols, bias, labels);
         p.lse = lse;
         p.weight = weight;
         p.dz = (unsigned char *)(ws + l.dz);
         p.dz_dx = (unsigned char *)(ws + l.dz_dx);
         p.dz_ld = (size_t)psteps * 256;
-        p.least_x = least;
-        p.least_w = least + 1 + k;
+        p.lows_x = (const int *)(ws + l.xlows);
+        p.lows_w = (const int *)(ws + l.wlows);
+        p.num_x = low_groups(up(d->N, 64) * 64);
+        p.num_w = low_groups(cols);
+        p.least = least;
         p.dbias = db ? (float *)(ws + l.strips) : nullptr;
+        if (!l.laid && k == 0) p.copy = from.x_rows(x, labels, nullptr, false);
         hipError_t e = launch(l.half, p.splits > 1 ? SM_PRODUCT_Z : SM_PRODUCT_DZ, l.z.tile, p, s);
         if (e != hipSuccess) return launched(e);
         if (p.splits > 1) {
@@ -663,10 +659,10 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
             if (l.half) hipLaunchKernelGGL(sm_split_dz_kernel<true>, grid, dim3(256), 0, s, p);
             else hipLaunchKernelGGL(sm_split_dz_kernel<false>, grid, dim3(256), 0, s, p);
         }
-        if (db) hipLaunchKernelGGL(sm_dbias_kernel, dim3(groups_of(cols)), dim3(256), 0, s, p.dbias, strips_of(l.z, d->N), cols, alpha, beta, db + v0);
 
+        SmParams qx = none;
         if (dx) {
-            SmParams q = none;
+            SmParams &q = qx;
             q.a = {l.half ? p.dz_dx : p.dz, p.dz_ld, 256, d->N, 0, 2};
             q.b = SmSource::across(wo, cols, l.isteps);
             q.M = d->N;
@@ -677,29 +673,40 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
             q.classes = d->O_total;
             q.weight = weight;
             q.alpha = 1.f;
-            q.least = p.least_w;
+            q.under = least + 1;
             q.partial = p.partial;
             float *sums = l.half ? (float *)dx : (float *)(ws + l.dxs);
             const bool last = k == l.pieces - 1;
             q.add = k ? sums : nullptr;
             q.out = last ? dx : sums;
             q.bf16 = last && !l.half;
-            if ((e = results(l.half, SM_PRODUCT_DX, q, l.dx, s)) != hipSuccess) return launched(e);
+            lay_tiles(q, l.dx);
         }
         SmParams q = none;
         q.a = {p.dz, p.dz_ld, 64 * p.dz_ld, d->N, 8 * psteps, 2};
-        q.b = SmSource::across(xo, nsteps * 64, l.isteps);
+        q.b = SmSource::across(from.along(ws + l.x, d->N), nsteps * 64, l.isteps);
         q.M = cols;
         q.N = d->I;
         q.products = products;
         q.steps = nsteps * products;
         q.alpha = alpha;
         q.beta = beta;
-        q.least = least;
+        q.under = least;
         q.partial = p.partial;
         q.out = dw + (size_t)v0 * d->I;
         q.big = (size_t)ol * d->I * 4 > (32u << 20);
-        if ((e = results(l.half, SM_PRODUCT_DW, q, l.dw, s)) != hipSuccess) return launched(e);
+        q.dbias = p.dbias;
+        q.strips = strips_of(l.z, d->N);
+        q.db = db ? db + v0 : nullptr;
+        lay_tiles(q, l.dw);
+        if (dx && l.pair != SM_NOTHING) {
+            e = l.half ? owt_launch_softmax_half_pair(l.pair, qx, q, qx.steps_per_split >= q.steps, s) : owt_launch_softmax_bf16_pair(l.pair, qx, q, qx.steps_per_split >= q.steps, s);
+            if (e != hipSuccess) return launched(e);
+            if (qx.splits > 1) join_parts(l.half, qx, s);
+        } else {
+            if (dx && (e = results(l.half, SM_PRODUCT_DX, qx, l.dx, s)) != hipSuccess) return launched(e);
+            if ((e = results(l.half, SM_PRODUCT_DW, q, l.dw, s)) != hipSuccess) return launched(e);
+        }
     }
     return launched();
 }

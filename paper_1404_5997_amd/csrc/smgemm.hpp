@@ -68,6 +68,17 @@ struct SmOperand {
 
 enum { SM_ONE = 1, SM_PAIR = 2, SM_THREE = 3 };     // products of a step of memory: one; both planes of A with B; the three larger of both planes of both
 
+// Rows of x or w laid out for the products: whole steps of 64 values, zeros behind the last one, and zeros for rows without a class (labels null: all have one).
+struct SmPrep {
+    const void *from;           // [rows][cols]
+    unsigned char *to;          // out_rows rows of `steps` steps
+    int rows, out_rows, cols, steps;
+    const int *labels;
+    int classes;
+    const float *weight;        // of the rows, or null
+    int *exps, *lows;           // fp32: each row's exponent, and the least of a work-group's rows, less those of their weights
+};
+
 struct SmParams {
     SmOperand a, b;
     int M, N;               // C
@@ -82,19 +93,24 @@ struct SmParams {
     Top *top;
     float *target;
     // backward: the whole layer's lse, weights or null; dz [M][step][2][64] (f16 values: one for dw and one for dx, with the least exponent of x's rows with their
-    // weights and that of w's rows), sums over the rows of each wavefront [..][N]
+    // weights and that of w's rows)
     const float *lse, *weight;
     unsigned char *dz, *dz_dx;
     size_t dz_ld;
-    const int *least_x, *least_w;
-    float *dbias;
+    const int *lows_x, *lows_w; // what the least exponents are the least of
+    int num_x, num_w;
+    int *least;                 // [0] of x, [1] of w: for the products that follow
+    SmPrep copy;                // bf16: x for dw, by work-groups behind the tiles' (out_rows 0: none)
+    float *dbias;               // sums over the rows of each wavefront [..][N]; dw: [strips][M], summed up to db
+    int strips;
+    float *db;
     // results
     void *out;              // C, rows of N values
     int bf16;               // its type
     int big;                // it is more than an eighth of the 256 MB behind the L2 caches
     float alpha, beta;      // beta only where results are fp32
     const float *add;       // fp32 [M][N] that is added to alpha times the sum (may be out), or null
-    const int *least;       // (f16 values) results are the sums times 2^-(*least + kSmDzTop)
+    const int *under;       // (f16 values) results are the sums times 2^-(*under + kSmDzTop)
     float *partial;         // [splits][M][N] (splits > 1)
 };
 constexpr int kSmTop = 14;          // a row's largest magnitude is scaled to [2^14, 2^15)
@@ -194,9 +210,34 @@ __device__ __forceinline__ void sm_put_bf16s(unsigned char *to, const float (&v)
     *(uint2 *)to = hi;
     *(uint2 *)(to + 128) = make_uint2(f32x2_to_bf16x2(lo[0], lo[1]), f32x2_to_bf16x2(lo[2], lo[3]));
 }
+// The least exponents of x's rows with their weights and of w's, found by the work-group for itself; `first` leaves them to the products that follow.
+// two: eight words of LDS that nothing else is in.
+__device__ __forceinline__ int2 sm_leasts(const SmParams &p, int *two, bool first)
+{
+    int x = kSmNone, w = kSmNone;
+    for (int i = threadIdx.x; i < p.num_x; i += 256) x = min(x, p.lows_x[i]);
+    for (int i = threadIdx.x; i < p.num_w; i += 256) w = min(w, p.lows_w[i]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+        x = min(x, __shfl_xor(x, d, 64));
+        w = min(w, __shfl_xor(w, d, 64));
+    }
+    if ((threadIdx.x & 63) == 0) {
+        two[threadIdx.x >> 6] = x;
+        two[4 + (threadIdx.x >> 6)] = w;
+    }
+    __syncthreads();
+    const int2 v = make_int2(min(min(two[0], two[1]), min(two[2], two[3])), min(min(two[4], two[5]), min(two[6], two[7])));
+    if (first && threadIdx.x == 0) {
+        p.least[0] = v.x;
+        p.least[1] = v.y;
+    }
+    return v;
+}
+
 // STARTED: sums that began at bias - lse / 2.  All lanes of a wavefront come here together.
 template <bool SCALED, bool STARTED>
-__device__ __forceinline__ void sm_dz(const SmParams &p, int m, int c, const float4 &sum, const SmDzRow &w, const SmDzColumns &k, float (&sums)[4])
+__device__ __forceinline__ void sm_dz(const SmParams &p, int2 least, int m, int c, const float4 &sum, const SmDzRow &w, const SmDzColumns &k, float (&sums)[4])
 {
     const float u[4] = {sum.x, sum.y, sum.z, sum.w};
     float d[4], e[4];
@@ -216,7 +257,7 @@ __device__ __forceinline__ void sm_dz(const SmParams &p, int m, int c, const flo
     if (m >= p.M || c >= (p.N + 63) / 64 * 64) return;
     const size_t at = (size_t)m * p.dz_ld + (size_t)(c >> 6) * 256 + 2 * (c & 63);
     if (SCALED) {
-        const int ex = kSmDzTop - (w.exp - *p.least_x), lw = *p.least_w + kSmDzTop;
+        const int ex = kSmDzTop - (w.exp - least.x), lw = least.y + kSmDzTop;
 #pragma unroll
         for (int t = 0; t < 4; t++) {
             d[t] = ldexpf(d[t], ex);
@@ -246,6 +287,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     typedef SmTile<TA, BM, NW> LoadA;
     typedef SmTile<TB, BN, NW> LoadB;
     constexpr int AI = LoadA::LOADS, BI = LoadB::LOADS, L = AI + BI;
+    static_assert(NW == 4, "256 threads");
     static_assert(NS >= 2 && (NS - 1) * L <= 63, "the wait counter has six bits");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -486,7 +528,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     // Results go through LDS, 32 rows of a wavefront at a time, so that rows are written as runs of 32 NB values; 16-byte piece q of row r sits in
     // slot q ^ (r % 16) (or % 8).  What a row has to itself comes from LDS, too: read from memory it would wait for the stores before it.
     constexpr int QW = 8 * NB, SW = QW < 16 ? QW - 1 : 15, RI = 64 / QW;        // pieces of a wavefront's row, the bits of a row's swizzle, rows of an access
-    static_assert(NS * STAGE >= NW * 32 * QW * 16 + BM * 16, "32 rows of each wavefront and what rows have to themselves fit the stages");
+    static_assert(NS * STAGE >= NW * 32 * QW * 16 + BM * 16 + 32, "32 rows of each wavefront and what rows have to themselves fit the stages");
     unsigned char *mine = lds + wave * (32 * QW * 16);
     const int q = lane % QW, c = n0 + wn0 + 4 * q;
     auto in_order = [] __attribute__((always_inline)) () {
@@ -519,6 +561,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
             label[r] = w.label;
             if (SCALED) rexp[r] = w.exp;
         }
+        const int2 least = SCALED ? sm_leasts(p, rexp + BM, tile == 0) : make_int2(0, 0);
         __syncthreads();
         const SmDzColumns k = sm_dz_columns<SCALED>(p, c);
         float sums[4] = {0.f, 0.f, 0.f, 0.f};
@@ -529,7 +572,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
             for (int r = 0; r < 32; r += RI) {
                 const int row = 32 * i + r + lane / QW;
                 const SmDzRow w = {lses[wm0 + row], weights[wm0 + row], label[wm0 + row], SCALED ? rexp[wm0 + row] : 0};
-                sm_dz<SCALED, STARTED>(p, m0 + wm0 + row, c, get_row(r), w, k, sums);
+                sm_dz<SCALED, STARTED>(p, least, m0 + wm0 + row, c, get_row(r), w, k, sums);
             }
         }
         if (p.dbias) {
@@ -550,7 +593,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
         const unsigned width = (unsigned)p.N * (!parts && p.bf16 ? 2 : 4);
         float *factor = (float *)(lds + NW * (32 * QW * 16));
         for (int r = tid; r < BM; r += 64 * NW) factor[r] = sm_row_factor<SCALED>(p, m0 + r);
-        const int shift = SCALED && !parts ? -(*p.least + kSmDzTop) : 0;
+        const int shift = SCALED && !parts ? -(*p.under + kSmDzTop) : 0;
         __syncthreads();
         char *base = (parts ? (char *)(p.partial + (size_t)split * p.M * p.N) : (char *)p.out) + (size_t)(m0 + wm0) * width;
         const int m_end = __builtin_amdgcn_readfirstlane(max(0, min(32 * MB, p.M - m0 - wm0)));     // rows of this wavefront that exist
@@ -615,16 +658,77 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
         };
         if ((p.N & 3) == 0) with(std::true_type{});
         else with(std::false_type{});
+        if (TA && p.db && n0 == 0 && split == 0)         // dw: rows are classes, and their bias has a gradient, too
+            for (int m = m0 + tid; m < min(m0 + BM, p.M); m += 64 * NW) {
+                float sum = 0.f;
+#pragma unroll 8
+                for (int k = 0; k < p.strips; k++) sum += p.dbias[(size_t)k * p.M + m];
+                p.db[m] = p.alpha * sum + (p.beta != 0.f ? p.beta * p.db[m] : 0.f);
+            }
     }
 }
+
+// 16 bytes from where rows begin anywhere
+struct __attribute__((packed, aligned(2))) SmLoose { uint32_t u[4]; };
+
+// bf16 rows, eight values a thread: work-group `at` of `of`
+__device__ __forceinline__ void sm_copy_rows(const SmPrep &p, int at, int of)
+{
+    const int pieces = p.steps * 8, blocks = (pieces + 255) / 256;      // work-groups of a row
+    for (int b = at; b < p.out_rows * blocks; b += of) {
+        const int m = b / blocks, i = (b - m * blocks) * 256 + threadIdx.x, c = 8 * i;
+        if (i >= pieces) continue;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (m < p.rows && c < p.cols && (!p.labels || has_class(p.labels[m], p.classes))) {
+            const uint16_t *row = (const uint16_t *)p.from + (size_t)m * p.cols;
+            if (c + 8 <= p.cols) {
+                const SmLoose l = *(const SmLoose *)(row + c);
+                v = make_uint4(l.u[0], l.u[1], l.u[2], l.u[3]);
+            } else {
+                uint32_t u[4];
+#pragma unroll
+                for (int k = 0; k < 4; k++) {
+                    const int e = c + 2 * k;
+                    u[k] = (e < p.cols ? row[e] : 0u) | ((e + 1 < p.cols ? (uint32_t)row[e + 1] : 0u) << 16);
+                }
+                v = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+        }
+        *(uint4 *)(p.to + (size_t)m * pieces * 16 + 16 * i) = v;
+    }
+}
+constexpr int kSmCopyGroups = 512;      // behind the tiles
 
 template <class Op, bool TA, bool TB, class S, int END>
 __global__ void __launch_bounds__(64 * S::NW, (S::OCC * S::NW + 3) / 4) sm_kernel(const SmParams p)
 {
     __shared__ __attribute__((aligned(16))) unsigned char lds[S::LDS];
+    if (!TA && !TB && END != SM_TOP && p.copy.out_rows) {
+        const int tiles = owt_split_major_grid(p.tiles, p.splits);
+        if ((int)blockIdx.x >= tiles) {
+            sm_copy_rows(p.copy, blockIdx.x - tiles, gridDim.x - tiles);
+            return;
+        }
+    }
     int tile, split;
     if (!owt_split_major_wg(p.tiles, p.splits, tile, split)) return;
     sm_tile<Op, TA, TB, S, END>(p, tile, split, lds);
+}
+
+// dx and dw in one launch, the one of longer sums first (dw is not split)
+template <class Op, class S>
+__global__ void __launch_bounds__(64 * S::NW, (S::OCC * S::NW + 3) / 4) sm_pair_kernel(const SmParams x, const SmParams w, bool x_first)
+{
+    __shared__ __attribute__((aligned(16))) unsigned char lds[S::LDS];
+    const int gx = owt_split_major_grid(x.tiles, x.splits), gw = owt_split_major_grid(w.tiles, 1), b = (int)blockIdx.x;
+    const bool of_x = x_first ? b < gx : b >= gw;
+    // (the numbering of owt_split_major_wg, within a product's work-groups: their number is a multiple of 8)
+    const int l = of_x ? (x_first ? b : b - gw) : (x_first ? b - gx : b), total = of_x ? x.tiles * x.splits : w.tiles;
+    const int xcd = l & 7, jx = l >> 3, each = total >> 3, more = total & 7;
+    if (jx >= each + (xcd < more ? 1 : 0)) return;
+    const int one = xcd * each + min(xcd, more) + jx;
+    if (of_x) sm_tile<Op, false, true, S, SM_OUT>(x, one % x.tiles, one / x.tiles, lds);
+    else sm_tile<Op, true, true, S, SM_OUT>(w, one, 0, lds);
 }
 
 }  // namespace owt

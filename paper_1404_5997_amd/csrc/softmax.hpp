@@ -21,5 +21,8 @@ hipError_t owt_launch_softmax_bf16_ends(int product, int tile, const SmParams &,
 hipError_t owt_launch_softmax_bf16_out(int product, int tile, const SmParams &, hipStream_t);       // Z, DX, DW
 hipError_t owt_launch_softmax_half_ends(int product, int tile, const SmParams &, hipStream_t);
 hipError_t owt_launch_softmax_half_out(int product, int tile, const SmParams &, hipStream_t);
+// dx and dw together: 128 x 128 or 64 x 64
+hipError_t owt_launch_softmax_bf16_pair(int tile, const SmParams &x, const SmParams &w, bool x_first, hipStream_t);
+hipError_t owt_launch_softmax_half_pair(int tile, const SmParams &x, const SmParams &w, bool x_first, hipStream_t);
 
 }  // namespace owt

@@ -11,7 +11,8 @@ typedef SmBf16 Op;
 
 template <bool TA, bool TB, class S, int END> static hipError_t go(const SmParams &p, hipStream_t s)
 {
-    hipLaunchKernelGGL((sm_kernel<Op, TA, TB, S, END>), dim3((unsigned)owt_split_major_grid(p.tiles, p.splits)), dim3(64 * S::NW), 0, s, p);
+    hipLaunchKernelGGL((sm_kernel<Op, TA, TB, S, END>), dim3((unsigned)(owt_split_major_grid(p.tiles, p.splits) + (p.copy.out_rows ? kSmCopyGroups : 0))), dim3(64 * S::NW), 0,
+                       s, p);
     return hipGetLastError();
 }
 template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmParams &p, hipStream_t s)
@@ -45,5 +46,20 @@ hipError_t OWT_INST_NAME(int product, int tile, const SmParams &p, hipStream_t s
 #endif
     return hipErrorInvalidValue;
 }
+
+#if OWT_INST_OUT
+#if OWT_INST_HALF
+hipError_t owt_launch_softmax_half_pair(int tile, const SmParams &x, const SmParams &w, bool x_first, hipStream_t s)
+#else
+hipError_t owt_launch_softmax_bf16_pair(int tile, const SmParams &x, const SmParams &w, bool x_first, hipStream_t s)
+#endif
+{
+    const dim3 grid((unsigned)(owt_split_major_grid(x.tiles, x.splits) + owt_split_major_grid(w.tiles, 1)));
+    if (tile == SM_MID) hipLaunchKernelGGL((sm_pair_kernel<Op, SmMid>), grid, dim3(256), 0, s, x, w, x_first);
+    else if (tile == SM_SMALL) hipLaunchKernelGGL((sm_pair_kernel<Op, SmSmall>), grid, dim3(256), 0, s, x, w, x_first);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+#endif
 
 }  // namespace owt

@@ -324,7 +324,7 @@ TILES = {"256x256": 120, "128x128": 121, "128x128, two a CU": 122, "64x64": 123}
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("splits", [1, 3])
+@pytest.mark.parametrize("splits", [0, 1, 3])      # as planned (dx and dw then perhaps in one launch), none, three
 @pytest.mark.parametrize("tile", TILES)
 @pytest.mark.parametrize("N,I,O", [(5, 130, 70), (300, 256, 600), (520, 72, 1030), (129, 1024, 257)])
 def test_tiles_and_splits(N, I, O, tile, splits, dt):
