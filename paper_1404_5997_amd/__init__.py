@@ -372,15 +372,17 @@ class tensor_list:
         self.at = (ctypes.c_void_p * max(1, self.count))(*[_ptr(t) for t in self.tensors])
         self.n = (ctypes.c_size_t * max(1, self.count))(*self.sizes)
 
-    def like(self, other, width):
-        """Whether this list has tensors of other's sizes, of values of `width` bytes."""
-        return self.sizes == other.sizes and (self.width == width or not self.count)
 
-
-def _lists(dtype, first, *others):
+def _lists(dtype, first, others=(), copies=None):
+    """Lists of one size and type (copies in bf16): what a call reads or writes of one has to exist in all."""
     width = 2 if dtype == OWT_BF16 else 4
-    if not all(l.like(first, w) for l, w in ((first, width),) + tuple((l, width) if not isinstance(l, tuple) else l for l in others)):
-        raise ValueError("lists of different sizes or types")
+    if first.count and first.width != width:
+        raise ValueError("lists of other values than the call's")
+    for l in others:
+        if l.sizes != first.sizes or l.width != first.width:
+            raise ValueError("lists of different sizes or types")
+    if copies is not None and (copies.sizes != first.sizes or (copies.count and copies.width != 2)):
+        raise ValueError("copies of other sizes, or not in bf16")
 
 
 def owt_grad_norm_workspace_bytes(g):
@@ -397,11 +399,11 @@ def owt_grad_norm(g, dtype, norm, ws=None, stream=None):
 
 
 def owt_grad_clip(g, out, dtype, norm, max_norm, stream=None):
-    _lists(dtype, g, out)
+    _lists(dtype, g, (out,))
     _check(_lib.owt_grad_clip(g.count, g.n, g.at, out.at, dtype, _ptr(norm), max_norm, _stream(stream)))
 
 
 def owt_sgd_momentum_clipped(w, vel, g, mu, eps, omega, gscale, norm, max_norm, w_bf16=None, stream=None):
-    _lists(OWT_F32, w, vel, g, *([(w_bf16, 2)] if w_bf16 is not None else []))
+    _lists(OWT_F32, w, (vel, g), w_bf16)
     _check(_lib.owt_sgd_momentum_clipped(w.count, w.n, w.at, vel.at, g.at, mu, eps, omega, gscale, _ptr(norm), max_norm,
                                          None if w_bf16 is None else w_bf16.at, _stream(stream)))

@@ -11,8 +11,10 @@
 namespace owt {
 
 constexpr int kClipGroups = 2048;       // eight work-groups of 256 threads a CU: all that run at a time
-constexpr int kSet = 80;                // tensors of a launch: with four pointers each 3.6 KB of arguments
+constexpr int kSet = 80;                // tensors of a launch (128 at most: walk_chunks): with four pointers each 3.6 KB of arguments
 constexpr int kChunkBytes = 16384;      // of gradients: 64 bytes a thread
+constexpr size_t kOneGroup = 4;         // so few chunks are one work-group's, and the launch that joins the sums is saved
+constexpr size_t kPastChunks = 8192;    // a list of more than 128 MB is written past the caches
 
 // P pointers for each tensor; chunks [first[t], first[t + 1]) are tensor t's, and its last one has last[t] values.  Work-group b has each + (b < more)
 // chunks.  (All in 32 bits: compared in 64, the size that is left was taken for a whole chunk by the compiler's choice between the two.)
@@ -23,18 +25,43 @@ template <int P> struct TensorSet {
     unsigned each, more;
 };
 
-// f(t, from, values) for each chunk of this work-group's run, `chunk` values at most
-template <int P, class F> __device__ __forceinline__ void walk_chunks(const TensorSet<P> &s, unsigned chunk, F f)
+// f(t, from, values) for each chunk of this work-group's run, `chunk` values at most.  BACK: from the run's end to its beginning.  The norm walks forwards and
+// leaves the ends of the runs in the 256 MB behind the L2 caches; who reads the gradients after it begins there.
+template <bool BACK, int P, class F> __device__ __forceinline__ void walk_chunks(const TensorSet<P> &s, unsigned chunk, F f)
 {
-    const unsigned b = blockIdx.x;
-    unsigned c = b * s.each + min(b, s.more);
-    const unsigned end = c + s.each + (b < s.more ? 1 : 0);
-    int t = 0;
-    for (; c < end; c++) {
-        while (c >= s.first[t + 1]) t++;
+    const unsigned b = blockIdx.x, begin = b * s.each + min(b, s.more), end = begin + s.each + (b < s.more ? 1 : 0);
+    // the tensor of the first chunk: how many begin there or before, counted by a wavefront at once (one after the other, or by halves, took 3 us a launch)
+    const unsigned from = BACK ? end - 1 : begin, lane = threadIdx.x & 63;
+    const unsigned a = lane < (unsigned)s.count ? s.first[lane] : ~0u, z = lane + 64 < (unsigned)s.count ? s.first[lane + 64] : ~0u;
+    int t = __builtin_amdgcn_readfirstlane(__popcll(__ballot(a <= from)) + __popcll(__ballot(z <= from)) - 1);
+    for (unsigned k = begin; k < end; k++) {
+        const unsigned c = BACK ? end - 1 - (k - begin) : k;
+        if (BACK)
+            while (c < s.first[t]) t--;
+        else
+            while (c >= s.first[t + 1]) t++;
         const unsigned n = c + 1 == s.first[t + 1] ? s.last[t] : chunk;
         f(t, (size_t)(c - s.first[t]) * chunk, n);
     }
+}
+// 16 and 8 bytes; PAST: by the caches, where there is more than they hold
+typedef unsigned clip_u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned clip_u32x2 __attribute__((ext_vector_type(2)));
+template <bool PAST> __device__ __forceinline__ void put(void *to, const uint4 &v)
+{
+    const clip_u32x4 u = {v.x, v.y, v.z, v.w};
+    if (PAST) __builtin_nontemporal_store(u, (clip_u32x4 *)to);
+    else *(clip_u32x4 *)to = u;
+}
+template <bool PAST> __device__ __forceinline__ void put(void *to, const uint2 &v)
+{
+    const clip_u32x2 u = {v.x, v.y};
+    if (PAST) __builtin_nontemporal_store(u, (clip_u32x2 *)to);
+    else *(clip_u32x2 *)to = u;
+}
+template <bool PAST> __device__ __forceinline__ void put(void *to, const float4 &v)
+{
+    put<PAST>(to, make_uint4(__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)));
 }
 
 template <class T> constexpr int kPer = 16 / sizeof(T);             // values of an access
@@ -86,7 +113,7 @@ __global__ void __launch_bounds__(64 * WAVES) grad_square_kernel(const TensorSet
 #pragma unroll
         for (int k = 0; k < V; k++) sum[k & 3] = fma((double)f[k], (double)f[k], sum[k & 3]);
     };
-    walk_chunks(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
+    walk_chunks<false>(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
         const T *g = (const T *)s.at[0][t] + from;
         if (n == CH) {
             uint4 v[U];
@@ -119,7 +146,7 @@ __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *part
 }
 
 // out = g * min(1, max / norm); zeros where the norm is not finite.  Gradients that stay as they are and where they are are not touched.
-template <class T>
+template <class T, bool PAST>
 __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, const float *norm, float max_norm)
 {
     constexpr int V = kPer<T>, CH = kChunkBytes / sizeof(T), U = CH / (V * 256);
@@ -133,7 +160,7 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, co
         for (int k = 0; k < V; k++) f[k] = fine ? f[k] * factor : 0.f;
         return narrow<T>(f);
     };
-    walk_chunks(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
+    walk_chunks<true>(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
         const T *g = (const T *)s.at[0][t] + from;
         T *out = (T *)s.at[1][t] + from;
         if (factor == 1.f && g == out) return;
@@ -142,7 +169,7 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, co
 #pragma unroll
             for (int u = 0; u < U; u++) v[u] = ((const uint4 *)g)[threadIdx.x + 256 * u];
 #pragma unroll
-            for (int u = 0; u < U; u++) ((uint4 *)out)[threadIdx.x + 256 * u] = scaled(v[u]);
+            for (int u = 0; u < U; u++) put<PAST>((uint4 *)out + threadIdx.x + 256 * u, scaled(v[u]));
         } else {
             for (unsigned i = threadIdx.x; i < n / V; i += 256) ((uint4 *)out)[i] = scaled(((const uint4 *)g)[i]);
             const unsigned i = n / V * V + threadIdx.x;
@@ -152,7 +179,7 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, co
 }
 
 // vel := mu*vel + eps*(gscale*factor*g - omega*w);  w := w + vel;  factor = min(1, max / (|gscale| norm)).  A norm that is not finite: no step.
-template <bool COPY>
+template <bool COPY, bool PAST>
 __global__ void __launch_bounds__(256) sgd_clipped_kernel(const TensorSet<3 + COPY> s, float mu, float eps, float omega, float gscale,
                                                           const float *norm, float max_norm)
 {
@@ -165,15 +192,15 @@ __global__ void __launch_bounds__(256) sgd_clipped_kernel(const TensorSet<3 + CO
         vv = fmaf(mu, vv, eps * fmaf(scale, gv, -omega * wv));
         wv += vv;
     };
-    walk_chunks(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
+    walk_chunks<true>(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
         float *w = (float *)s.at[0][t] + from, *vel = (float *)s.at[1][t] + from;
         const float *g = (const float *)s.at[2][t] + from;
         uint16_t *wb = COPY ? (uint16_t *)s.at[2 + COPY][t] + from : nullptr;
-        auto put = [&](unsigned i, float4 a, float4 v, const float4 &d) __attribute__((always_inline)) {
+        auto step = [&](unsigned i, float4 a, float4 v, const float4 &d) __attribute__((always_inline)) {
             upd(a.x, v.x, d.x); upd(a.y, v.y, d.y); upd(a.z, v.z, d.z); upd(a.w, v.w, d.w);
-            ((float4 *)vel)[i] = v;
-            ((float4 *)w)[i] = a;
-            if (COPY) ((uint2 *)wb)[i] = make_uint2(f32x2_to_bf16x2(a.x, a.y), f32x2_to_bf16x2(a.z, a.w));
+            put<PAST>((float4 *)vel + i, v);
+            put<PAST>((float4 *)w + i, a);
+            if (COPY) put<PAST>((uint2 *)wb + i, make_uint2(f32x2_to_bf16x2(a.x, a.y), f32x2_to_bf16x2(a.z, a.w)));
         };
         if (n == CH) {
             float4 a[U], v[U], d[U];
@@ -184,9 +211,9 @@ __global__ void __launch_bounds__(256) sgd_clipped_kernel(const TensorSet<3 + CO
                 d[u] = ((const float4 *)g)[threadIdx.x + 256 * u];
             }
 #pragma unroll
-            for (int u = 0; u < U; u++) put(threadIdx.x + 256 * u, a[u], v[u], d[u]);
+            for (int u = 0; u < U; u++) step(threadIdx.x + 256 * u, a[u], v[u], d[u]);
         } else {
-            for (unsigned i = threadIdx.x; i < n / 4; i += 256) put(i, ((const float4 *)w)[i], ((const float4 *)vel)[i], ((const float4 *)g)[i]);
+            for (unsigned i = threadIdx.x; i < n / 4; i += 256) step(i, ((const float4 *)w)[i], ((const float4 *)vel)[i], ((const float4 *)g)[i]);
             const unsigned i = n / 4 * 4 + threadIdx.x;
             if (i < n) {
                 float a = w[i], v = vel[i];
@@ -286,11 +313,18 @@ owt_status owt_grad_norm(int count, const size_t *n, const void *const *g, owt_d
     hipStream_t s = (hipStream_t)hip_stream;
     double *partial = (double *)ws;
     int parts = 0;
-    OWT_TRY(for_sets<1>(count, n, {g}, chunk, [&](const TensorSet<1> &set, unsigned groups) {
-        if (dtype == OWT_F32) hipLaunchKernelGGL((grad_square_kernel<float, 4>), dim3(groups), dim3(256), 0, s, set, partial + parts, (float *)nullptr);
-        else hipLaunchKernelGGL((grad_square_kernel<bf16_t, 4>), dim3(groups), dim3(256), 0, s, set, partial + parts, (float *)nullptr);
+    const bool one = sets == 1 && chunks <= kOneGroup;
+    OWT_TRY(for_sets<1>(count, n, {g}, chunk, [&](TensorSet<1> &set, unsigned groups) {
+        if (one) {
+            set.each = (unsigned)chunks;
+            set.more = 0;
+            groups = 1;
+        }
+        if (dtype == OWT_F32) hipLaunchKernelGGL((grad_square_kernel<float, 4>), dim3(groups), dim3(256), 0, s, set, partial + parts, one ? norm : nullptr);
+        else hipLaunchKernelGGL((grad_square_kernel<bf16_t, 4>), dim3(groups), dim3(256), 0, s, set, partial + parts, one ? norm : nullptr);
         parts += (int)groups;
     }));
+    if (one) return OWT_OK;
     hipLaunchKernelGGL(grad_norm_join_kernel, dim3(1), dim3(1024), 0, s, partial, parts, norm);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? OWT_OK : fail(OWT_ELAUNCH, "HIP launch failed: %s", hipGetErrorString(e));
@@ -315,8 +349,11 @@ owt_status owt_grad_clip(int count, const size_t *n, const void *const *g, void 
     OWT_TRY(check_bound(norm, max_norm));
     hipStream_t s = (hipStream_t)hip_stream;
     return for_sets<2>(count, n, {g, out}, chunk, [&](const TensorSet<2> &set, unsigned groups) {
-        if (dtype == OWT_F32) hipLaunchKernelGGL(grad_clip_kernel<float>, dim3(groups), dim3(256), 0, s, set, norm, max_norm);
-        else hipLaunchKernelGGL(grad_clip_kernel<bf16_t>, dim3(groups), dim3(256), 0, s, set, norm, max_norm);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, set, norm, max_norm); };
+        const bool past = chunks > kPastChunks;
+        if (dtype == OWT_F32) { if (past) go(grad_clip_kernel<float, true>); else go(grad_clip_kernel<float, false>); }
+        else if (past) go(grad_clip_kernel<bf16_t, true>);
+        else go(grad_clip_kernel<bf16_t, false>);
     });
 }
 
@@ -335,12 +372,17 @@ owt_status owt_sgd_momentum_clipped(int count, const size_t *n, float *const *w,
     OWT_TRY(check_bound(norm, max_norm));
     hipStream_t s = (hipStream_t)hip_stream;
     const void *const *W = (const void *const *)w, *const *V = (const void *const *)vel, *const *G = (const void *const *)g;
+    const bool past = chunks > kPastChunks / 2;         // (two lists are written)
     if (w_bf16_or_null)
         return for_sets<4>(count, n, {W, V, G, w_bf16_or_null}, chunk, [&](const TensorSet<4> &set, unsigned groups) {
-            hipLaunchKernelGGL(sgd_clipped_kernel<true>, dim3(groups), dim3(256), 0, s, set, mu, eps, omega, gscale, norm, max_norm);
+            auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, set, mu, eps, omega, gscale, norm, max_norm); };
+            if (past) go(sgd_clipped_kernel<true, true>);
+            else go(sgd_clipped_kernel<true, false>);
         });
     return for_sets<3>(count, n, {W, V, G}, chunk, [&](const TensorSet<3> &set, unsigned groups) {
-        hipLaunchKernelGGL(sgd_clipped_kernel<false>, dim3(groups), dim3(256), 0, s, set, mu, eps, omega, gscale, norm, max_norm);
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(groups), dim3(256), 0, s, set, mu, eps, omega, gscale, norm, max_norm); };
+        if (past) go(sgd_clipped_kernel<false, true>);
+        else go(sgd_clipped_kernel<false, false>);
     });
 }
 

@@ -9,7 +9,7 @@ from gpu_util import owt, workspace  # noqa: E402
 
 U = 2.0 ** -24
 # one value, nothing, sizes about a chunk of 16 KB and its accesses, more tensors than a launch takes
-LISTS = [[], [0], [1], [0, 3, 0], [4095, 4096, 4097], [8191, 8192, 8193, 1], [7] * 200, [5000, 0, 70001] * 60, [1 << 20, 3, (1 << 21) + 5]]
+LISTS = [[], [0], [1], [0, 3, 0], [4095, 4096, 4097], [8191, 8192, 8193, 1], [7] * 200, [4096, 8192, 4095], [4, 3], [5000, 0, 70001] * 60, [1 << 20, 3, (1 << 21) + 5]]
 
 
 def make(sizes, dtype, seed, scale=1.0):
