@@ -141,9 +141,13 @@ __device__ __forceinline__ void sm_load_lds(unsigned off, const unsigned char *b
 
 enum { SM_TOP, SM_DZ, SM_OUT };
 
-template <int WM_, int WN_, int MB_, int NB_, int NS_, int OCC_> struct SmShape {
-    static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, NS = NS_, OCC = OCC_, NW = WM * WN, BM = 32 * MB * WM, BN = 32 * NB * WN;
-    static constexpr int STAGE = (BM + BN) * 128, RING = NS * STAGE, LDS = RING + (BM + BN) * 4;
+// RING: 0, NS stages of both operands' tiles of a step.  SM_PAIR, SM_THREE: the products of a step of memory go together, and LDS holds five tiles of one
+// operand, filled one by one in the order they are used.  256 x 256 results take 32 KB of either operand a step, so that two stages are all that LDS holds; this way a
+// step of memory loads three tiles for two products, or four for three, instead of four and six, a tile that two products use is read from LDS once and stays in
+// registers for the other, and a load has two products to arrive in.
+template <int WM_, int WN_, int MB_, int NB_, int NS_, int OCC_, int RING_ = 0> struct SmShape {
+    static constexpr int WM = WM_, WN = WN_, MB = MB_, NB = NB_, NS = NS_, OCC = OCC_, RING = RING_, NW = WM * WN, BM = 32 * MB * WM, BN = 32 * NB * WN;
+    static constexpr int STAGE = RING_ ? BM * 128 : (BM + BN) * 128, TILES = NS * STAGE, LDS = TILES + (RING_ ? 0 : (BM + BN) * 4);
 };
 
 // The pieces of a tile of R rows of C that a lane loads, and where a fragment's lane reads.
@@ -288,7 +292,8 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     typedef SmTile<TB, BN, NW> LoadB;
     constexpr int AI = LoadA::LOADS, BI = LoadB::LOADS, L = AI + BI;
     static_assert(NW == 4, "256 threads");
-    static_assert(NS >= 2 && (NS - 1) * L <= 63, "the wait counter has six bits");
+    static_assert(S::RING || (NS >= 2 && (NS - 1) * L <= 63), "the wait counter has six bits");
+    static_assert(!S::RING || (BM == BN && NS == 5 && 3 * AI <= 63), "tiles of one size, five of them");
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int li = lane & 31, lh = lane >> 5;
@@ -363,7 +368,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     };
 
     const bool some = END != SM_OUT || nst > 0;     // (split sums alone may have none here)
-    if (some)
+    if (!S::RING && some)
 #pragma unroll
         for (int s = 0; s < NS; s++) {
             aim(s_beg + s, s);
@@ -377,7 +382,7 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     constexpr bool SCALED = std::is_same<Op, SmHalf>::value, STARTED = !SCALED && END != SM_OUT;
     sm_f32x16 acc[MB][NB];
     if (STARTED) {
-        float *bias = (float *)(lds + S::RING), *half = bias + BN;      // (each read from memory once, and not by every lane for itself: 45 us of 250 in a launch of 512 tiles)
+        float *bias = (float *)(lds + S::TILES), *half = bias + BN;      // (each read from memory once, and not by every lane for itself: 45 us of 250 in a launch of 512 tiles)
         for (int c = tid; c < BN; c += 64 * NW) bias[c] = n0 + c < p.N ? (p.bias ? p.bias[n0 + c] : 0.f) : -INFINITY;
         if (END == SM_DZ)
             for (int r = tid; r < BM; r += 64 * NW) half[r] = 0.5f * sm_dz_row<false>(p, m0 + r).lse;
@@ -438,7 +443,151 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
     // s_waitcnt vmcnt(n) lgkmcnt(0), expcnt untouched; then the same of all wavefronts
 #define OWT_ARRIVED(n) do { asm volatile("" ::: "memory"); __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | (7 << 4)); \
                             __builtin_amdgcn_s_barrier(); asm volatile("" ::: "memory"); } while (0)
-    if (some) {
+    if constexpr (S::RING != 0) {
+        // Tile n of the order in which they are used lies in slot n % 5.  Two products: B, A0, A1 of a step of memory; three: A1, B0, A0, B1 for A1 B0, A0 B0 and A0 B1.
+        // A product reads the fragments of the next slice between the instructions of one, its last slice the first ones of the next product; before that slice everybody has
+        // read the product's tiles, and those that no later product reads are filled anew.
+        constexpr bool THREE = S::RING == SM_THREE;
+        constexpr int PER = THREE ? 4 : 3, PRODUCTS = THREE ? 3 : 2;
+        const int t_beg = s_beg / PRODUCTS, t_end = t_beg + nst / PRODUCTS - 1;
+        sm_i32x4 keep_a[THREE ? 4 : 1][MB], keep_b[4][NB], roll[2][MB > NB ? MB : NB];      // (rolling: those of A1, or of the tile that one product uses)
+        int slot = 0;                               // of the step's first tile
+        auto place = [&](int j) __attribute__((always_inline)) { const int at = slot + j; return (at >= 5 ? at - 5 : at) * STAGE; };
+        const unsigned char *from_a, *from_b;       // where the tiles that are being loaded lie
+        auto aim_a = [&](int t, int plane) __attribute__((always_inline)) {
+            t = __builtin_amdgcn_readfirstlane(min(t, t_end));
+            if (TA && 64 * t + 64 > p.a.rows) {
+#pragma unroll
+                for (int i = 0; i < AI; i++) asrc[i] = LoadA::from(p.a, wave, lane, i, m0, p.a.rows - 64 * t);
+            }
+            from_a = sm_uniform(ag + (size_t)t * p.a.step + 128 * plane);
+        };
+        auto aim_b = [&](int t, int plane) __attribute__((always_inline)) {
+            t = __builtin_amdgcn_readfirstlane(min(t, t_end));
+            if (TB && 64 * t + 64 > p.b.rows) {
+#pragma unroll
+                for (int i = 0; i < BI; i++) bsrc[i] = LoadB::from(p.b, wave, lane, i, n0, p.b.rows - 64 * t);
+            }
+            from_b = sm_uniform(bg + (size_t)t * p.b.step + 128 * plane);
+        };
+        auto load_a = [&](int i, int at) __attribute__((always_inline)) { sm_load_lds(asrc[i < AI ? i : 0], from_a, lds0 + at + NW * i * 1024); };
+        auto load_b = [&](int i, int at) __attribute__((always_inline)) { sm_load_lds(bsrc[i < BI ? i : 0], from_b, lds0 + at + NW * i * 1024); };
+        auto read_a = [&](sm_i32x4 &to, int at, int kc, int f) __attribute__((always_inline)) {
+            if (TA) to = read_across(at + kc * 32 * BM + acrossA[f], 2 * BM);
+            else to = *(const sm_i32x4 *)(lds + at + (wm0 + 32 * f) * 128 + along[kc]);
+        };
+        auto read_b = [&](sm_i32x4 &to, int at, int kc, int f) __attribute__((always_inline)) {
+            if (TB) to = read_across(at + kc * 32 * BN + acrossB[f], 2 * BN);
+            else to = *(const sm_i32x4 *)(lds + at + (wn0 + 32 * f) * 128 + along[kc]);
+        };
+        // products of a and b; reads f = 0 .. reads - 1, loads i = 0 .. loads - 1
+        auto together = [&](const sm_i32x4 (&a)[MB], const sm_i32x4 (&b)[NB], int reads, auto reader, int loads, auto loader) __attribute__((always_inline)) {
+#pragma unroll
+            for (int t = 0; t < P; t++) {
+#pragma unroll
+                for (int f = 0; f < MB + NB; f++)
+                    if (f < reads && f * P / reads == t) reader(f);
+                acc[t / NB][t % NB] = Op::mul(b[t % NB], a[t / NB], acc[t / NB][t % NB]);
+#pragma unroll
+                for (int i = 0; i < 2 * AI; i++)
+                    if (i < loads && i * P / loads == t) loader(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto nothing = [](int) __attribute__((always_inline)) {};
+        if (some) {
+#pragma unroll
+            for (int n = 0; n < 5; n++) {
+                const int t = t_beg + n / PER, j = n % PER;
+                const bool of_b = THREE ? (j & 1) : j == 0;
+                if (of_b) aim_b(t, THREE && j == 3);
+                else aim_a(t, THREE ? j == 0 : j - 1);
+#pragma unroll
+                for (int i = 0; i < AI; i++) {
+                    if (of_b) load_b(i, n * STAGE);
+                    else load_a(i, n * STAGE);
+                }
+            }
+            OWT_ARRIVED(3 * AI);
+            if constexpr (THREE) {
+#pragma unroll
+                for (int f = 0; f < MB; f++) read_a(roll[0][f], place(0), 0, f);
+#pragma unroll
+                for (int f = 0; f < NB; f++) read_b(keep_b[0][f], place(1), 0, f);
+                int t = t_beg;
+                do {
+                    // A1 B0
+#pragma unroll
+                    for (int kc = 0; kc < 3; kc++)
+                        together(roll[kc & 1], keep_b[kc], MB + NB, [&](int f) __attribute__((always_inline)) {
+                            if (f < MB) read_a(roll[(kc & 1) ^ 1][f < MB ? f : 0], place(0), kc + 1, f < MB ? f : 0);
+                            else read_b(keep_b[kc + 1][f < MB ? 0 : f - MB], place(1), kc + 1, f < MB ? 0 : f - MB);
+                        }, 0, nothing);
+                    OWT_ARRIVED(2 * AI);            // A0 is there; A1 and B0 have been read: B0 and A0 of the next step come in their places
+                    aim_b(t + 1, 0);
+                    aim_a(t + 1, 0);
+                    together(roll[1], keep_b[3], MB, [&](int f) __attribute__((always_inline)) { read_a(keep_a[0][f < MB ? f : 0], place(2), 0, f < MB ? f : 0); },
+                             2 * AI, [&](int i) __attribute__((always_inline)) {
+                                 if (i < BI) load_b(i, place(0));
+                                 else load_a(i - BI, place(1));
+                             });
+                    // A0 B0
+#pragma unroll
+                    for (int kc = 0; kc < 3; kc++)
+                        together(keep_a[kc], keep_b[kc], MB, [&](int f) __attribute__((always_inline)) { read_a(keep_a[kc + 1][f < MB ? f : 0], place(2), kc + 1, f < MB ? f : 0); }, 0, nothing);
+                    OWT_ARRIVED(3 * AI);            // B1 is there; A0 has been read: B1 of the next step
+                    aim_b(t + 1, 1);
+                    together(keep_a[3], keep_b[3], NB, [&](int f) __attribute__((always_inline)) { read_b(roll[0][f < NB ? f : 0], place(3), 0, f < NB ? f : 0); },
+                             BI, [&](int i) __attribute__((always_inline)) { load_b(i, place(2)); });
+                    // A0 B1
+#pragma unroll
+                    for (int kc = 0; kc < 3; kc++)
+                        together(keep_a[kc], roll[kc & 1], NB, [&](int f) __attribute__((always_inline)) { read_b(roll[(kc & 1) ^ 1][f < NB ? f : 0], place(3), kc + 1, f < NB ? f : 0); }, 0, nothing);
+                    OWT_ARRIVED(2 * AI);            // the next step's A1 and B0 are there; B1 has been read: A1 of the step after that
+                    aim_a(t + 2, 1);
+                    together(keep_a[3], roll[1], MB + NB, [&](int f) __attribute__((always_inline)) {
+                        if (f < MB) read_a(roll[0][f < MB ? f : 0], place(4), 0, f < MB ? f : 0);
+                        else read_b(keep_b[0][f < MB ? 0 : f - MB], place(0), 0, f < MB ? 0 : f - MB);
+                    }, AI, [&](int i) __attribute__((always_inline)) { load_a(i, place(3)); });
+                    slot = slot + 4 >= 5 ? slot - 1 : slot + 4;
+                } while (++t <= t_end);
+            } else {
+#pragma unroll
+                for (int f = 0; f < MB; f++) read_a(roll[0][f], place(1), 0, f);
+#pragma unroll
+                for (int f = 0; f < NB; f++) read_b(keep_b[0][f], place(0), 0, f);
+                int t = t_beg;
+                do {
+                    // A0 B
+#pragma unroll
+                    for (int kc = 0; kc < 3; kc++)
+                        together(roll[kc & 1], keep_b[kc], MB + NB, [&](int f) __attribute__((always_inline)) {
+                            if (f < MB) read_a(roll[(kc & 1) ^ 1][f < MB ? f : 0], place(1), kc + 1, f < MB ? f : 0);
+                            else read_b(keep_b[kc + 1][f < MB ? 0 : f - MB], place(0), kc + 1, f < MB ? 0 : f - MB);
+                        }, 0, nothing);
+                    OWT_ARRIVED(2 * AI);            // A1 is there; A0 and B have been read: A1 of the next step and B of the one after that come in the places of B and A0
+                    aim_a(t + 1, 1);
+                    aim_b(t + 2, 0);
+                    together(roll[1], keep_b[3], MB, [&](int f) __attribute__((always_inline)) { read_a(roll[0][f < MB ? f : 0], place(2), 0, f < MB ? f : 0); },
+                             2 * AI, [&](int i) __attribute__((always_inline)) {
+                                 if (i < AI) load_a(i, place(0));
+                                 else load_b(i - AI, place(1));
+                             });
+                    // A1 B
+#pragma unroll
+                    for (int kc = 0; kc < 3; kc++)
+                        together(roll[kc & 1], keep_b[kc], MB, [&](int f) __attribute__((always_inline)) { read_a(roll[(kc & 1) ^ 1][f < MB ? f : 0], place(2), kc + 1, f < MB ? f : 0); }, 0, nothing);
+                    OWT_ARRIVED(2 * AI);            // the next step's B and A0 are there; A1 has been read: A0 of the step after that
+                    aim_a(t + 2, 0);
+                    together(roll[1], keep_b[3], MB + NB, [&](int f) __attribute__((always_inline)) {
+                        if (f < MB) read_a(roll[0][f < MB ? f : 0], place(4), 0, f < MB ? f : 0);
+                        else read_b(keep_b[0][f < MB ? 0 : f - MB], place(3), 0, f < MB ? 0 : f - MB);
+                    }, AI, [&](int i) __attribute__((always_inline)) { load_a(i, place(2)); });
+                    slot = slot + 3 >= 5 ? slot - 2 : slot + 3;
+                } while (++t <= t_end);
+            }
+        }
+    } else if (some) {
         OWT_ARRIVED(STARTED ? 0 : (NS - 1) * L);    // (with what the sums started from, everything)
 #pragma unroll
         for (int f = 0; f < MB + NB; f++) read(0, 0, 0, f);

@@ -9,6 +9,9 @@ namespace owt {
 // The pair of 128 x 128 covers one another's beginnings and ends where there are enough of them, the single one has more on its way where there are few (us, one and the
 // other: outputs of 777 rows 1536 -> 20000, 1104 tiles, 86 and 69, their dx, 88 tiles, 161 and 210).  256 x 128 and 32 x 256 were never the fastest.
 typedef SmShape<2, 2, 4, 4, 2, 1> SmBig;
+typedef SmShape<2, 2, 4, 4, 5, 1, SM_PAIR> SmBigPair;        // (256 x 256, too: where more than kSmRing steps of memory have several products)
+typedef SmShape<2, 2, 4, 4, 5, 1, SM_THREE> SmBigThree;
+constexpr int kSmRing = 4;
 typedef SmShape<2, 2, 2, 2, 3, 1> SmMid;
 typedef SmShape<2, 2, 2, 2, 2, 2> SmPair;
 typedef SmShape<2, 2, 1, 1, 4, 2> SmSmall;

@@ -17,7 +17,16 @@ template <bool TA, bool TB, class S, int END> static hipError_t go(const SmParam
 }
 template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmParams &p, hipStream_t s)
 {
-    if (tile == SM_BIG) return go<TA, TB, SmBig, END>(p, s);
+    if (tile == SM_BIG) {
+        const bool ring = p.steps_per_split > kSmRing * p.products;
+#if OWT_INST_HALF
+        if (ring) return go<TA, TB, SmBigThree, END>(p, s);
+#else
+        if constexpr (TA)
+            if (ring) return go<TA, TB, SmBigPair, END>(p, s);
+#endif
+        return go<TA, TB, SmBig, END>(p, s);
+    }
     if (tile == SM_MID) return go<TA, TB, SmMid, END>(p, s);
     if (tile == SM_TWO) return go<TA, TB, SmPair, END>(p, s);
     if (tile == SM_SMALL) return go<TA, TB, SmSmall, END>(p, s);
