@@ -1,7 +1,11 @@
 """A stack of residual blocks of dense layers in 8 bits, forward, backward and update: how the calls on 8-bit rows are used together.
 
 A block is   h <- h + x;   u = relu(W1 norm(h) + b1);   x <- W2 u + b2   (x: what the block before it gave), and the stack ends in a norm and an
-output layer of logistic units.  Weights live as fp32 masters and as 8-bit rows, which the products read and every update writes anew.
+output layer.  Weights live as fp32 masters and as 8-bit rows, which the products read and every update writes anew.
+
+The output layer's units are logistic, or a softmax over the classes.  A softmax is trained without its outputs: the loss and its gradients come from the
+normed rows and the layer's weights, both in storage type, so that no buffer has rows of `classes` values however many there are.  A bound on the
+gradients' norm, where one is given, holds every step back to it.
 
 What a block keeps for its backward pass is h in storage type and, a byte a value, the 8-bit rows that its two products read: they are
 operand and checkpoint in one.  u itself is not kept.  Its ReLU mask is read back from the rows: a value that 8 bits took to zero gave
@@ -12,14 +16,19 @@ Buffers and call order only; every arithmetic step runs in the library's kernels
 import torch
 
 from . import (OWT_BF16, OWT_BIAS, OWT_F32, OWT_PASS_BWD_DATA, OWT_PASS_FWD, OWT_RELU, fc_desc, owt_fc_shard_q8_bwd, owt_fc_shard_q8_fwd,
-               owt_fc_shard_q8_workspace_bytes, owt_logistic_xent, owt_q8_pack, owt_q8_pitch, owt_q8_unpack, owt_rmsnorm_q8_bwd,
-               owt_rmsnorm_q8_fwd, owt_rmsnorm_q8_workspace_bytes, owt_sgd_momentum_update)
+               owt_fc_shard_q8_workspace_bytes, owt_fc_softmax_bwd, owt_fc_softmax_fwd, owt_fc_softmax_workspace_bytes, owt_grad_norm,
+               owt_grad_norm_workspace_bytes, owt_logistic_xent, owt_q8_pack, owt_q8_pitch, owt_q8_unpack, owt_rmsnorm_q8_bwd, owt_rmsnorm_q8_fwd,
+               owt_rmsnorm_q8_workspace_bytes, owt_sgd_momentum_clipped, owt_sgd_momentum_update, tensor_list)
 
 
 class Dense8Stack:
-    """N rows of `width` values through `blocks` blocks of `hidden` units, then `classes` logistic units."""
+    """N rows of `width` values through `blocks` blocks of `hidden` units, then `classes` units: "logistic" ones, or one "softmax" (labels outside
+    the classes are then rows that do not count).  max_norm bounds the norm of the gradients of a step (None: no bound)."""
 
-    def __init__(self, N, width, hidden, blocks, classes, dtype="bf16", eps=1e-5):
+    def __init__(self, N, width, hidden, blocks, classes, dtype="bf16", eps=1e-5, loss="logistic", max_norm=None):
+        if loss not in ("logistic", "softmax"):
+            raise ValueError("loss is logistic or softmax")
+        self.softmax, self.max_norm = loss == "softmax", max_norm
         self.N, self.width, self.hidden, self.classes, self.eps = N, width, hidden, classes, eps
         self.code = OWT_BF16 if dtype == "bf16" else OWT_F32
         self.tdt = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -35,13 +44,28 @@ class Dense8Stack:
             if len(self.blocks) < blocks:
                 b.update(q2=self._rows(hidden), s2=self._new((N,), torch.float32))
             self.blocks.append(b)
+        if self.softmax:
+            head = self.layers[-1]["desc"]
+            scratch = max([scratch] + [owt_fc_softmax_workspace_bytes(head, p) for p in (OWT_PASS_FWD, OWT_PASS_BWD_DATA)])
+            self.normed, self.lse = self._new((N, width)), self._new((N,), torch.float32)
         self._carve_parameters()
+        self.grad_norm = self._new((1,), torch.float32)
+        self._lists = tuple(tensor_list([a]) for a in (self.params, self.vel, self.grads))
+        self._copies = tensor_list([self.copies]) if self.copies is not None else None
+        scratch = max(scratch, owt_grad_norm_workspace_bytes(self._lists[2]))
         self.ws = self._new((max(16, scratch),), torch.uint8)
         self.x = self._new((N, width))          # input, and what a block adds to h
         self.u, self.du = self._new((N, hidden)), self._new((N, hidden))        # one of each for all blocks
         self.dn, self.dh = self._new((N, width)), self._new((N, width))
-        self.logits, self.loss = self._new((N, classes)), self._new((N,), torch.float32)
+        self._logits, self.loss = None, self._new((N,), torch.float32)
         self.labels = torch.zeros((N,), device="cuda", dtype=torch.int32)
+
+    @property
+    def logits(self):
+        """Outputs [N, classes]: made when they are first asked for, which training a softmax never does."""
+        if self._logits is None:
+            self._logits = self._new((self.N, self.classes))
+        return self._logits
 
     def _new(self, shape, dtype=None):
         return torch.empty(shape, device="cuda", dtype=self.tdt if dtype is None else dtype)
@@ -58,7 +82,11 @@ class Dense8Stack:
             slots.append((owner, name, shape, at, n))
             at += (n + 7) // 8 * 8              # every view 16-byte aligned
         self.params, self.grads, self.vel = (torch.zeros((at,), device="cuda", dtype=torch.float32) for _ in range(3))
+        # a softmax reads its layer's weights in storage type: in bf16 every update writes a copy
+        self.copies = torch.zeros((at,), device="cuda", dtype=torch.bfloat16) if self.softmax and self.tdt == torch.bfloat16 else None
         for owner, name, shape, o, n in slots:
+            if name == "w" and owner is self.layers[-1]:
+                owner["stored"] = (self.params if self.copies is None else self.copies)[o:o + n].view(shape)
             owner[name], owner["d" + name] = self.params[o:o + n].view(shape), self.grads[o:o + n].view(shape)
 
     def init(self, seed):
@@ -71,6 +99,12 @@ class Dense8Stack:
         self.pack_weights()
 
     def pack_weights(self):
+        """8-bit rows, and copies in storage type, of the masters as they are."""
+        if self.copies is not None:
+            self.copies.copy_(self.params)
+        self._pack_rows()
+
+    def _pack_rows(self):
         for e in self.layers:
             owt_q8_pack(e["O"], e["I"], OWT_F32, e["w"], e["wq"], e["ws"])
 
@@ -83,6 +117,13 @@ class Dense8Stack:
 
     def forward(self, x):
         """Logits [N, classes] of x [N, width] (its own buffer is not written)."""
+        self.trunk(x)
+        last = self.blocks[-1]
+        self._shard(self.layers[-1], last["q1"], last["s1"], self.logits)
+        return self.logits
+
+    def trunk(self, x):
+        """All blocks and the last norm: what the output layer reads."""
         N, last = self.N, None
         for i, b in enumerate(self.blocks):
             if i == 0:
@@ -95,8 +136,12 @@ class Dense8Stack:
                 owt_q8_pack(N, self.hidden, self.code, self.u, b["q2"], b["s2"])
                 self._shard(self.layers[2 * i + 1], b["q2"], b["s2"], self.x)
             last = b
-        self._shard(self.layers[-1], last["q1"], last["s1"], self.logits)
-        return self.logits
+
+    def softmax_loss(self):
+        """The losses of the rows that the trunk left, in self.loss."""
+        e, b = self.layers[-1], self.blocks[-1]
+        owt_q8_unpack(self.N, self.width, self.code, b["q1"], b["s1"], self.normed)
+        owt_fc_softmax_fwd(e["desc"], self.normed, e["stored"], e["b"], self.labels, self.lse, None, self.loss, self.ws)
 
     def _shard_back(self, e, q, s, mask, dy, dx):
         owt_fc_shard_q8_bwd(e["desc"], q, s, e["wq"], e["ws"], mask, dy, 1.0 / self.N, 0.0, dx, e["dw"], e["db"], self.ws)
@@ -104,7 +149,10 @@ class Dense8Stack:
     def backward(self):
         """Gradients (means over the rows) from the labels; the gradient of the input is left in self.dh."""
         N, code = self.N, self.code
-        owt_logistic_xent(N, self.classes, 0, code, self.logits, self.labels, 1.0, self.loss, self.logits)
+        if self.softmax:
+            self.softmax_loss()
+        else:
+            owt_logistic_xent(N, self.classes, 0, code, self.logits, self.labels, 1.0, self.loss, self.logits)
         for i in range(len(self.blocks) - 1, -1, -1):
             b = self.blocks[i]
             if "q2" in b:
@@ -114,17 +162,28 @@ class Dense8Stack:
                 owt_q8_unpack(N, self.hidden, code, b["q2"], b["s2"], self.u)
                 self._shard_back(w1, b["q1"], b["s1"], self.u, self.du, self.dn)
                 along = self.dh
+            elif self.softmax:
+                e, along = self.layers[-1], None
+                owt_fc_softmax_bwd(e["desc"], self.normed, e["stored"], e["b"], self.labels, self.lse, None, 1.0 / N, 0.0, self.dn, e["dw"], e["db"], self.ws)
             else:
                 self._shard_back(self.layers[-1], b["q1"], b["s1"], None, self.logits, self.dn)
                 along = None
             owt_rmsnorm_q8_bwd(N, self.width, code, self.dn, b["h"], b["gain"], b["rstd"], along, 1.0 / N, 0.0, self.dh, b["dgain"], self.ws)
 
     def update(self, mu, eps, omega):
-        owt_sgd_momentum_update(self.params.numel(), self.params, self.vel, self.grads, mu, eps, omega, -1.0)
-        self.pack_weights()
+        if self.max_norm is None:
+            owt_sgd_momentum_update(self.params.numel(), self.params, self.vel, self.grads, mu, eps, omega, -1.0, self.copies)
+        else:
+            w, vel, g = self._lists
+            owt_grad_norm(g, OWT_F32, self.grad_norm, self.ws)
+            owt_sgd_momentum_clipped(w, vel, g, mu, eps, omega, -1.0, self.grad_norm, self.max_norm, self._copies)
+        self._pack_rows()
 
     def step(self, x, labels, mu=0.9, eps=0.01, omega=0.0005):
         self.labels.copy_(labels)
-        self.forward(x)
+        if self.softmax:
+            self.trunk(x)
+        else:
+            self.forward(x)
         self.backward()
         self.update(mu, eps, omega)

@@ -14,8 +14,8 @@ import torch
 
 from . import (OWT_BF16, OWT_BIAS, OWT_F32, OWT_PASS_BWD_DATA, OWT_PASS_BWD_FILTER, OWT_PASS_FWD, OWT_RELU,
                conv_desc, fc_desc, owt_conv_autotune, owt_conv_bwd_data, owt_conv_bwd_data_relu_in, owt_conv_bwd_filter, owt_conv_fwd, owt_conv_workspace_bytes,
-               owt_fc_autotune, owt_fc_shard_bwd, owt_fc_shard_fwd, owt_fc_workspace_bytes, owt_logistic_xent, owt_maxpool_bwd_relu,
-               owt_maxpool_fwd, owt_sgd_momentum_update)
+               owt_fc_autotune, owt_fc_shard_bwd, owt_fc_shard_fwd, owt_fc_workspace_bytes, owt_grad_norm, owt_grad_norm_workspace_bytes,
+               owt_logistic_xent, owt_maxpool_bwd_relu, owt_maxpool_fwd, owt_sgd_momentum_clipped, owt_sgd_momentum_update, tensor_list)
 
 
 class ConvStack:
@@ -107,6 +107,7 @@ class ConvStack:
         self.grads = torch.zeros((off,), device=dev, dtype=torch.float32)
         self.vel = torch.zeros((off,), device=dev, dtype=torch.float32)
         self.params_bf16 = torch.zeros((off,), device=dev, dtype=torch.bfloat16) if self.dt == "bf16" else None
+        self.grad_norm, self._lists = torch.zeros((1,), device=dev, dtype=torch.float32), {}        # of bounded updates
         for e, key, shape, o, n in slots:
             e[key + "32"] = self.params[o:o + n].view(shape)                 # fp32 master
             e["d" + key] = self.grads[o:o + n].view(shape)
@@ -115,12 +116,21 @@ class ConvStack:
             else:
                 e[key] = e[key + "32"]
 
-    def update(self, mu, eps, omega, gscale=-1.0, part="all"):
+    def update(self, mu, eps, omega, gscale=-1.0, part="all", max_norm=None):
         """Weight update rule of Section 5 over every parameter of the worker (or only the convolution
         / dense part of the array), one launch.  The gradients in self.grads are batch means of a loss
-        (alpha = 1/N), so the default gscale = -1 descends."""
+        (alpha = 1/N), so the default gscale = -1 descends.  With max_norm the norm of that part's gradients
+        is taken first, left in self.grad_norm, and bounds the step; where it is not finite there is none."""
         lo, hi = {"all": (0, self.n_params), "conv": (0, self.fc_offset), "fc": (self.fc_offset, self.n_params)}[part]
-        if hi > lo:
+        if hi > lo and max_norm is not None:
+            if part not in self._lists:
+                of = lambda a: None if a is None else tensor_list([a[lo:hi]])   # noqa: E731
+                w, vel, g, copy = (of(a) for a in (self.params, self.vel, self.grads, self.params_bf16))
+                self._lists[part] = w, vel, g, copy, torch.empty((max(16, owt_grad_norm_workspace_bytes(g)),), device=self.params.device, dtype=torch.uint8)
+            w, vel, g, copy, ws = self._lists[part]
+            self._run("norm " + part, owt_grad_norm, g, OWT_F32, self.grad_norm, ws)
+            self._run("sgd update " + part, owt_sgd_momentum_clipped, w, vel, g, mu, eps, omega, gscale, self.grad_norm, max_norm, copy)
+        elif hi > lo:
             self._run("sgd update " + part, owt_sgd_momentum_update, hi - lo, self.params[lo:hi], self.vel[lo:hi],
                       self.grads[lo:hi], mu, eps, omega, gscale,
                       None if self.params_bf16 is None else self.params_bf16[lo:hi])

@@ -1,6 +1,7 @@
 """Trains a small stack of 8-bit dense blocks (paper_1404_5997_amd/dense8.py) on rows around class centres, then serves single rows with it.
 
     python train_dense8.py [--rows 1024 --width 1024 --hidden 4096 --blocks 4 --classes 125 --steps 200 --rate 0.02 --dtype bf16]
+                           [--loss softmax --max-norm 1.0]
 """
 import argparse
 
@@ -16,6 +17,13 @@ def at_least_one(text):
     return n
 
 
+def above_zero(text):
+    v = float(text)
+    if not v > 0.0:
+        raise argparse.ArgumentTypeError("%s is not greater than zero" % text)
+    return v
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description="Trains a small stack of 8-bit dense blocks and serves single rows with it.")
     for name, default in (("rows", 1024), ("width", 1024), ("hidden", 4096), ("classes", 125), ("steps", 200)):
@@ -23,9 +31,11 @@ def main(argv=None):
     ap.add_argument("--blocks", type=int, default=4)
     ap.add_argument("--rate", type=float, default=0.02)
     ap.add_argument("--dtype", choices=("f32", "bf16"), default="bf16")
+    ap.add_argument("--loss", choices=("logistic", "softmax"), default="logistic")
+    ap.add_argument("--max-norm", type=above_zero, default=None, help="bound on the norm of a step's gradients")
     a = ap.parse_args(argv)
     g = torch.Generator(device="cuda").manual_seed(1)
-    net = Dense8Stack(a.rows, a.width, a.hidden, a.blocks, a.classes, a.dtype)
+    net = Dense8Stack(a.rows, a.width, a.hidden, a.blocks, a.classes, a.dtype, loss=a.loss, max_norm=a.max_norm)
     net.init(0)
     centres = torch.randn((a.classes, a.width), generator=g, device="cuda")
     for k in range(a.steps):
@@ -33,7 +43,8 @@ def main(argv=None):
         x = (centres[labels.long()] + 0.5 * torch.randn((a.rows, a.width), generator=g, device="cuda")).to(net.tdt)
         net.step(x, labels, eps=a.rate)
         if k % 25 == 0 or k == a.steps - 1:
-            print("step %d: loss %.4f" % (k, net.loss.mean().item()), flush=True)
+            norm = "" if a.max_norm is None else ", gradients %.4f" % net.grad_norm.item()
+            print("step %d: loss %.4f%s" % (k, net.loss.mean().item(), norm), flush=True)
     whole = a.rows * ((a.blocks + 1) * 2 * a.width + a.blocks * a.hidden) * net.x.element_size()     # (the last norm has no hidden rows behind it)
     print("kept for the backward pass: %.1f MB (in storage type it would be %.1f)" % (net.checkpoint_bytes() / 1e6, whole / 1e6))
     one = Dense8Stack(1, a.width, a.hidden, a.blocks, a.classes, a.dtype)      # a served row: the trained weights, one row at a time
