@@ -86,7 +86,12 @@ template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(cons
 // ------------------------------------------------------------------------------------------------ after the products
 
 __device__ __forceinline__ float lse_of(Top t) { return (__builtin_isfinite(t.max) ? t.max : 0.f) + logf(t.sum); }
-__device__ __forceinline__ float loss_of(float lse, float target) { return target == -INFINITY ? INFINITY : lse - target; }
+// lse - target without lse's own rounding, which is what is left of a small loss: a label whose output is the largest, 10, and a loss of 0.05 lose five digits in 10.05 - 10
+__device__ __forceinline__ float loss_of(Top t, float target)
+{
+    if (target == -INFINITY) return INFINITY;
+    return __builtin_isfinite(t.max) ? (t.max - target) + logf(t.sum) : lse_of(t) - target;
+}
 
 struct SmRows {                 // what is known of rows of outputs, and where it goes
     const Top *top;             // [parts][N]
@@ -104,7 +109,7 @@ __device__ __forceinline__ void finish_row(const SmRows &p, int n, Top t, const 
         if (!has_class(label, p.classes)) lse = target = 0.f;
         else {
             if (label >= p.off && label - p.off < p.cols) target = *label_out;
-            loss = loss_of(lse, target);
+            loss = loss_of(t, target);
         }
         if (p.target) p.target[n] = target;
         if (p.loss) p.loss[n] = loss;
@@ -263,7 +268,7 @@ __global__ void __launch_bounds__(256) softmax_join_kernel(int workers, int N, i
     const float l = lse_of(t);
     lse[n] = l;
     if (target) target[n] = at;
-    if (loss) loss[n] = loss_of(l, at);
+    if (loss) loss[n] = loss_of(t, at);
 }
 
 // ------------------------------------------------------------------------------------------------ host
@@ -378,9 +383,33 @@ struct SmLayout {
         laid = half || I % 64;
         products = half ? SM_THREE : SM_ONE;
         const size_t row = (size_t)isteps * (half ? 256 : 128);
-        piece = forward ? forward_piece(laid, row, ol) : backward_piece(laid, half, N, row, ol);
-        pieces = ol ? up(ol, piece) : 0;
-        z = sm_plan(N, piece, isteps * products, products, !forward);
+        auto plans = [&](int cols) {
+            piece = cols;
+            pieces = up(ol, cols);
+            z = sm_plan(N, cols, isteps * products, products, !forward);
+            if (forward) return;
+            dx = sm_plan(N, I, up(cols, 64) * products, products, false);
+            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), half ? SM_THREE : SM_PAIR, false);
+        };
+        auto us = [&] { return (float)pieces * (z.us + dx.us + dw.us); };
+        if (forward) plans(forward_piece(laid, row, ol));
+        else {
+            plans(backward_piece(laid, half, N, row, ol, 0));
+            // Pieces whose tiles come in whole rounds of the chip: of 4096 rows, 4096 -> 65536, eight of 8192 classes take 7.16 ms, six of up to 12288 7.5, eleven 8.1.
+            const int fewest = pieces;
+            if (fewest > 1) {
+                int best = piece;
+                float least_us = us();
+                for (int more = 1; more <= fewest && more <= 6; more++) {
+                    plans(backward_piece(laid, half, N, row, ol, more));
+                    if (us() < 0.98f * least_us) {
+                        least_us = us();
+                        best = piece;
+                    }
+                }
+                plans(best);
+            }
+        }
         if (forward && pieces > 1) z.splits = 1;        // (a split row's outputs are joined in one go)
         size_t at = 0;
         auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
@@ -394,7 +423,7 @@ struct SmLayout {
         least = take(half && !forward ? 8 : 0);
         pair = SM_NOTHING;
         top = label_out = dz = dz_dx = dxs = strips = partial = total = 0;
-        dx = dw = z;
+        if (forward) dx = dw = z;
         if (z.tile < 0) return;
         size_t parts = partial_bytes(z, N, piece);
         if (forward) {
@@ -402,8 +431,6 @@ struct SmLayout {
             label_out = take((size_t)N * 4);
         } else {
             const int psteps = up(piece, 64);
-            dx = sm_plan(N, I, psteps * (half ? SM_THREE : SM_ONE), half ? SM_THREE : SM_ONE, false);
-            dw = sm_plan(piece, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), half ? SM_THREE : SM_PAIR, false);
             dz = take((size_t)N * psteps * 256);
             dz_dx = take(half ? (size_t)N * psteps * 256 : 0);
             dxs = take(!half && pieces > 1 ? (size_t)N * I * 4 : 0);
@@ -422,20 +449,20 @@ struct SmLayout {
     }
     bool fits() const { return z.tile >= 0 && dx.tile >= 0 && dw.tile >= 0; }
     // Classes of a piece: as many as `fit`, but pieces alike
-    static int alike(size_t fit, size_t least, int ol)
+    static int alike(size_t fit, size_t least, int ol, int more = 0)
     {
         fit = fit < least ? least : fit;
         if (fit >= (size_t)ol) return ol;
-        const int pieces = (int)((ol + fit - 1) / fit);
+        const int pieces = (int)((ol + fit - 1) / fit) + more;
         return up(up(ol, pieces), 256) * 256;
     }
     // Weights that are laid out go in pieces of at most 256 MB; outputs are not kept, so that the others are one piece.
     static int forward_piece(bool laid, size_t row, int ol) { return laid ? alike(((size_t)256 << 20) / row, 256, ol) : ol; }
     // dz, and weights that are laid out, stay in the 256 MB behind the L2 caches between the product that writes them and those that read them
-    static int backward_piece(bool laid, bool half, int N, size_t row, int ol)
+    static int backward_piece(bool laid, bool half, int N, size_t row, int ol, int more)
     {
         const size_t each = (size_t)N * (half ? 8 : 4) + (laid ? row : 0);
-        return alike(((size_t)128 << 20) / (each ? each : 1), 1024, ol);
+        return alike(((size_t)128 << 20) / (each ? each : 1), 1024, ol, more);
     }
 };
 
