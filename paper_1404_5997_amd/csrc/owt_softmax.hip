@@ -24,8 +24,8 @@ __global__ void __launch_bounds__(256) sm_rows_kernel(const SmPrep a, const SmPr
     else sm_copy_rows(b, blockIdx.x - groups_a, gridDim.x - groups_a);
 }
 
-// fp32 rows as two f16 values under the power of two that brings a row's largest magnitude to [2^14, 2^15), ROWS rows a work-group.  A row is read twice,
-// the second time from the caches.  Four rows a work-group for many rows, one for few.
+// fp32 rows as two f16 values under the power of two that brings a row's largest magnitude to [2^14, 2^15), ROWS rows a work-group.  What a
+// thread does not keep of a row (1024 values of it, or 4096) is read twice, the second time from the caches.  Four rows a work-group for many rows, one for few.
 template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(const SmPrep a, const SmPrep b, int groups_a)
 {
     constexpr int EACH = 256 / ROWS;        // threads of a row
@@ -46,13 +46,19 @@ template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(cons
         }
         return make_float4(row[c], c + 1 < p.cols ? row[c + 1] : 0.f, c + 2 < p.cols ? row[c + 2] : 0.f, 0.f);
     };
+    constexpr int HELD = 4;                 // pieces of four that a thread keeps
+    float4 held[HELD];
     float most = 0.f;
+    auto size = [&](const float4 &v) __attribute__((always_inline)) {
+        most = fmaxf(fmaxf(fmaxf(most, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
+    };
+#pragma unroll
+    for (int k = 0; k < HELD; k++) held[k] = four(4 * at + 4 * EACH * k);
+#pragma unroll
+    for (int k = 0; k < HELD; k++) size(held[k]);
     if (real)
 #pragma unroll 4
-        for (int c = 4 * at; c < p.cols; c += 4 * EACH) {
-            const float4 v = four(c);
-            most = fmaxf(fmaxf(fmaxf(most, fabsf(v.x)), fmaxf(fabsf(v.y), fabsf(v.z))), fabsf(v.w));
-        }
+        for (int c = 4 * at + 4 * EACH * HELD; c < p.cols; c += 4 * EACH) size(four(c));
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) most = fmaxf(most, __shfl_xor(most, d, 64));
     if (ROWS == 1) {
@@ -64,12 +70,15 @@ template <int ROWS> __global__ void __launch_bounds__(256) sm_halves_kernel(cons
     const int exp = !(most > 0.f) ? kSmNone : __builtin_isfinite(most) ? kSmTop - ilogbf(most) : 0, shift = exp == kSmNone ? 0 : exp;
     if (m < p.out_rows) {
         unsigned char *to = p.to + (size_t)m * p.steps * 256;
-#pragma unroll 4
-        for (int c = 4 * at; c < p.steps * 64; c += 4 * EACH) {
-            const float4 v = four(c);
+        auto write = [&](int c, const float4 &v) __attribute__((always_inline)) {
             const float s[4] = {ldexpf(v.x, shift), ldexpf(v.y, shift), ldexpf(v.z, shift), ldexpf(v.w, shift)};
             sm_put_halves(to + (size_t)(c >> 6) * 256 + 2 * (c & 63), s);
-        }
+        };
+#pragma unroll
+        for (int k = 0; k < HELD; k++)
+            if (4 * at + 4 * EACH * k < p.steps * 64) write(4 * at + 4 * EACH * k, held[k]);
+#pragma unroll 4
+        for (int c = 4 * at + 4 * EACH * HELD; c < p.steps * 64; c += 4 * EACH) write(c, four(c));
         if (at == 0 && m < p.rows) p.exps[m] = exp;
     }
     if (!p.lows) return;                    // (of all threads, or of none)
@@ -144,14 +153,28 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_top_kerne
     const float *row = p.partial + (size_t)m * p.N;
     const int re = SCALED ? p.row_exp[m] : 0;
     Top t = {-INFINITY, 0.f};
-    for (int c = threadIdx.x; c < p.N; c += 256) {
-        float z = 0.f;
+    const bool vec = (p.N & 3) == 0;
+    for (int c = 4 * threadIdx.x; c < p.N; c += 1024) {
+        float z[4] = {0.f, 0.f, 0.f, 0.f};
+        if (vec) {
+#pragma unroll 8
+            for (int k = 0; k < p.splits; k++) {
+                const float4 v = *(const float4 *)(row + k * whole + c);
+                z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w;
+            }
+        } else
 #pragma unroll 4
-        for (int k = 0; k < p.splits; k++) z += row[k * whole + c];
-        if (SCALED) z = ldexpf(z, -(re + p.col_exp[c]));
-        if (p.bias) z += p.bias[c];
-        if (c == at) label_out = z;
-        t = join(t, top_of(z));
+            for (int k = 0; k < p.splits; k++)
+#pragma unroll
+                for (int i = 0; i < 4; i++) z[i] += c + i < p.N ? row[k * whole + c + i] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; i++)
+            if (c + i < p.N) {
+                if (SCALED) z[i] = ldexpf(z[i], -(re + p.col_exp[c + i]));
+                if (p.bias) z[i] += p.bias[c + i];
+                if (c + i == at) label_out = z[i];
+                t = join(t, top_of(z[i]));
+            }
     }
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) t = join(t, {__shfl_xor(t.max, d, 64), __shfl_xor(t.sum, d, 64)});
@@ -175,7 +198,7 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_split_dz_kernel
         const float *row = p.partial + (size_t)m * p.N + c;
         if ((p.N & 3) == 0) {
             if (c < p.N && m < p.M)
-#pragma unroll 4
+#pragma unroll 8
                 for (int s = 0; s < p.splits; s++) {
                     const float4 v = *(const float4 *)(row + s * whole);
                     z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w;
@@ -312,8 +335,8 @@ constexpr int SM_NOTHING = -1;          // more work-groups than a launch holds
 struct SmPlan { int tile, splits; float us; };
 static int up(int n, int to) { return (n + to - 1) / to; }
 
-// A product of M x N results and `steps` steps, `products` of which stay together; dz: they leave as dz
-static SmPlan sm_plan(long M, long N, int steps, int products, bool dz)
+// A product of M x N results and `steps` steps, `products` of which stay together; end: how they leave
+static SmPlan sm_plan(long M, long N, int steps, int products, int end)
 {
     SmPlan best{SM_NOTHING, 1, 1e30f};
     const int want = forced_tile() - kSmFirstTile, want_split = forced_split(), most = steps / products;
@@ -324,9 +347,11 @@ static SmPlan sm_plan(long M, long N, int steps, int products, bool dz)
         if (!groups_fit(tiles, 256)) continue;
         for (int sp = 1; sp <= 32 && (sp == 1 || (sp * 2 <= most && tiles * sp <= 1024)); sp *= 2) {
             const long n = tiles * sp;
-            const float step = n >= (t == SM_BIG ? 192 : 128) ? q.busy : q.step, one = q.start + (dz && sp == 1 ? q.dz : 0.f) + (float)(up(most, sp) * products) * step;
+            const float step = n >= (t == SM_BIG ? 192 : 128) ? q.busy : q.step, one = q.start + (end == SM_DZ && sp == 1 ? q.dz : 0.f) + (float)(up(most, sp) * products) * step;
+            const float out = end != SM_OUT && sp == 1 ? 0.f : (float)(q.bm * q.bn) * 4.f / 17.6e3f;      // written at a CU's share of the memory's rate
+            const float work = one > out ? one : out;
             const float each = q.together > 1 && n > 256 ? (float)n / 256.f + 0.5f : (float)((n + 255) / 256);      // work-groups of a CU
-            float us = 3.f + each * (q.together > 1 && n <= 256 ? q.start + (one - q.start) * 1.2f : one);
+            float us = 3.f + each * (q.together > 1 && n <= 256 ? q.start + (work - q.start) * 1.2f : work);
             if (sp > 1) us += 3.6f + (float)(sp + 1) * (float)M * (float)N * 4.f / 3e6f;        // the launch that adds up
             if (us < best.us) best = {t, sp, us};
         }
@@ -386,10 +411,10 @@ struct SmLayout {
         auto plans = [&](int cols) {
             piece = cols;
             pieces = up(ol, cols);
-            z = sm_plan(N, cols, isteps * products, products, !forward);
+            z = sm_plan(N, cols, isteps * products, products, forward ? SM_TOP : SM_DZ);
             if (forward) return;
-            dx = sm_plan(N, I, up(cols, 64) * products, products, false);
-            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), half ? SM_THREE : SM_PAIR, false);
+            dx = sm_plan(N, I, up(cols, 64) * products, products, SM_OUT);
+            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), half ? SM_THREE : SM_PAIR, SM_OUT);
         };
         auto us = [&] { return (float)pieces * (z.us + dx.us + dw.us); };
         if (forward) plans(forward_piece(laid, row, ol));
@@ -721,7 +746,7 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
         q.under = least;
         q.partial = p.partial;
         q.out = dw + (size_t)v0 * d->I;
-        q.big = (size_t)ol * d->I * 4 > (32u << 20);
+        q.big = (size_t)ol * d->I * 4 > (32u << 20) && d->I % 32 == 0;        // (rows of whole lines of 128 bytes: parts of lines join in the caches)
         q.dbias = p.dbias;
         q.strips = strips_of(l.z, d->N);
         q.db = db ? db + v0 : nullptr;
