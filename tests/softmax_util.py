@@ -107,7 +107,7 @@ def assert_within(got, want, off, what):
     assert got.shape == want.shape, what
     same = np.isfinite(want)
     assert np.array_equal(got[~same], want[~same], equal_nan=True), "%s: %r where %r" % (what, got[~same][:4], want[~same][:4])
-    d = np.abs(got - want)[same]
+    d = np.abs(got[same] - want[same])
     lim = (off if np.ndim(off) else np.full(want.shape, off))[same] + 2.0 ** -126
     bad = ~(d <= lim)
     assert not bad.any(), "%s: %d of %d off, the worst %.3g where %.3g is allowed" % (what, bad.sum(), bad.size, d[bad].max(), lim[bad][np.argmax(d[bad])])

@@ -10,7 +10,8 @@ from softmax_util import Reference, assert_within, grads, inputs  # noqa: E402
 
 # rows, inputs, classes: one row, one class, sizes about tiles, steps and pieces, few rows of many classes, many rows of few
 SIZES = [(1, 64, 1000), (1, 1, 1), (2, 3, 5), (7, 65, 33), (32, 128, 257), (33, 192, 256), (64, 64, 64), (65, 63, 129), (128, 256, 1000), (130, 1000, 125),
-         (255, 130, 511), (256, 512, 512), (257, 72, 600), (300, 65, 4097), (515, 96, 10), (1000, 200, 2), (16, 2048, 3000), (3, 1537, 9001)]
+         (255, 130, 511), (256, 512, 512), (257, 72, 600), (300, 65, 4097), (515, 96, 10), (1000, 200, 2), (16, 2048, 3000), (3, 1537, 9001),
+         (700, 640, 5000), (2100, 328, 3000)]
 
 
 def code(dt):
@@ -356,3 +357,37 @@ def test_pieces(dt):
     got = run_bwd(N, I, O, dt, x, w, b, labels, l32, weight, 1.0 / N, 0.0, None, None)
     for k, (want, off) in grads(ref, l32, weight, dt, 1.0 / N, 0.0, None, None).items():
         assert_within(got[k], want, off, k)
+
+
+def test_weights_of_more_than_four_gigabytes():
+    """Offsets beyond 32 bits: rows at both ends and in the middle of 2 million classes."""
+    m = owt()
+    N, I, O = 3, 1024, 2_000_000
+    g = torch.Generator(device="cuda").manual_seed(1)
+    w = torch.empty((O, I), device="cuda", dtype=torch.bfloat16).normal_(0.0, 2.0 * I ** -0.5, generator=g)
+    x = torch.randn((N, I), generator=g, device="cuda").to(torch.bfloat16)
+    labels = torch.tensor([O - 1, 0, O // 2], device="cuda", dtype=torch.int32)
+    x = (x.float() + 4.0 * w[labels.long()].float()).to(torch.bfloat16)
+    d = m.fc_desc(N, I, O, 1, 0, m.OWT_BF16, 0)
+    lse, target, loss = (torch.empty((N,), device="cuda") for _ in range(3))
+    ws = workspace(max(m.owt_fc_softmax_workspace_bytes(d, p) for p in (0, 1)))
+    m.owt_fc_softmax_fwd(d, x, w, None, labels, lse, target, loss, ws)
+    dx, dw, db = torch.empty((N, I), device="cuda", dtype=torch.bfloat16), torch.full((O, I), float("nan"), device="cuda"), torch.full((O,), float("nan"), device="cuda")
+    m.owt_fc_softmax_bwd(d, x, w, None, labels, lse, None, 1.0, 0.0, dx, dw, db, ws)
+    torch.cuda.synchronize()
+    xd, dxr = x.double(), torch.zeros((N, I), device="cuda", dtype=torch.float64)
+    z = torch.cat([xd @ w[k:k + 100_000].double().t().contiguous() for k in range(0, O, 100_000)], 1)
+    want = torch.logsumexp(z, 1)
+    size = (xd.abs() @ w[:1000].double().abs().t().contiguous()).max().item() * 1.5         # (sums of magnitudes hardly differ from row to row of w)
+    off = 2.0 ** -23 * (I + 2) * size
+    assert ((lse - want).abs() <= off + 2.0 ** -17 + 2.0 ** -12).all()
+    assert ((target - z.gather(1, labels.long()[:, None])[:, 0]).abs() <= off).all()
+    p = torch.exp(z - lse.double()[:, None])
+    p.scatter_add_(1, labels.long()[:, None], torch.full((N, 1), -1.0, device="cuda", dtype=torch.float64))
+    rel = 2 * off + 2.0 ** -16                   # of an exponential: its output's error, and the two bf16 values that it leaves as
+    for k in range(0, O, 100_000):
+        dxr += p[:, k:k + 100_000].contiguous() @ w[k:k + 100_000].double()
+        wr = p[:, k:k + 100_000].t().contiguous() @ xd
+        assert ((dw[k:k + 100_000].double() - wr).abs() <= rel * (p[:, k:k + 100_000].abs() + 2.0 ** -30).t().contiguous() @ xd.abs() + rel * 1e-4).all(), k
+    assert ((db.double() - p.sum(0)).abs() <= rel * (p.abs().sum(0) + 1e-4)).all()
+    assert ((dx.double() - dxr).norm() <= 2.0 ** -8 * 2 * dxr.norm())
