@@ -174,8 +174,8 @@ template <bool ACROSS, int R, int NW> struct SmTile {
     }
 };
 
-// dz = weight (exp(z - lse) - [label]): what a row and four columns bring to it, and what is kept.  Rows without a class are zeros, and so are
-// columns past the last up to a whole step: an lse of infinity and a bias of -infinity take exponentials to zero.  (Rows all of whose outputs are -infinity
+// dz = weight (exp(z - lse) - [label]): what a row and four columns bring to it, and what is kept.  Rows without a class are zeros (they have no weight), and so are
+// columns past the last up to a whole step: a bias of -infinity takes exponentials to zero.  (Rows all of whose outputs are -infinity
 // have an lse of -infinity: any other number will do in its place.)
 struct SmDzRow { float lse, weight; int label, exp; };      // exp: of x's row
 struct SmDzColumns { float bias[4]; int exp[4]; };          // exp: of w's rows
@@ -255,7 +255,7 @@ __device__ __forceinline__ void sm_dz(const SmParams &p, int2 least, int m, int 
 #pragma unroll
     for (int t = 0; t < 4; t++) {
         const float from_lse = STARTED ? u[t] - 0.5f * w.lse : (SCALED ? ldexpf(u[t], -(w.exp + k.exp[t])) : u[t]) + k.bias[t] - w.lse;
-        e[t] = exp_of(from_lse);
+        e[t] = w.weight == 0.f ? 0.f : exp_of(from_lse);        // (a row without a class may hold anything, and bf16 outputs are of x as it lies)
     }
     if (__any((unsigned)(w.label - c) < 4u))        // (of many classes hardly ever)
 #pragma unroll

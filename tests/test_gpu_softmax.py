@@ -81,7 +81,7 @@ def test_what_is_not_wanted_is_left_out(dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("N,I,O", [(5, 40, 70), (300, 130, 520)])
+@pytest.mark.parametrize("N,I,O", [(5, 40, 70), (300, 130, 520), (5, 64, 70), (300, 128, 520), (520, 64, 2000), (40, 2048, 96)])
 def test_rows_without_a_class_have_no_influence(N, I, O, dt):
     x, w, b, labels, weight = inputs(N, I, O, 5, dt, nobody=0.3)
     labels[0], labels[-1] = -1, O
@@ -104,7 +104,7 @@ def test_rows_without_a_class_have_no_influence(N, I, O, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
-@pytest.mark.parametrize("N,I,O", [(3, 40, 70), (270, 64, 600)])
+@pytest.mark.parametrize("N,I,O", [(3, 40, 70), (270, 64, 600), (30, 2048, 130)])
 def test_classes_that_are_taken_out(N, I, O, dt):
     x, w, b, labels, _ = inputs(N, I, O, 6, dt, nobody=0.0)
     b[1::3] = -np.inf
