@@ -401,7 +401,8 @@ const char *owt_last_error(void);
  * forward, 92..94 forward / backward-data of layers of few tiles; 100..106 the bf16 filter gradient over images
  * that streams its operands into LDS; 110..112 the products of the dense shard in 8 bits,
  * 113 its forward product of few results, 114 its backward pass in one launch; 120..123 the products of softmax
- * cross-entropy: 256 x 256, 128 x 128, the same with two work-groups a CU, 64 x 64), `splitk` > 0 forces the
+ * cross-entropy: 256 x 256, 128 x 128, the same with two work-groups a CU, 64 x 64, 124 up to 64 fp32 rows with
+ * the weights as they lie), `splitk` > 0 forces the
  * split count of the reduction (clamped to the number of reduction steps), `flags` is a set of
  * OWT_FORCE_* bits.  While an override is active, tuned and cached plans are ignored.  The three
  * values are stored atomically, but a launch that runs concurrently with this call may see the old

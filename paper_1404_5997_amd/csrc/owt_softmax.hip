@@ -11,6 +11,7 @@
 // values as two f16 ones.
 #include <cmath>
 
+#include "smfew.hpp"
 #include "softmax.hpp"
 
 namespace owt {
@@ -391,8 +392,23 @@ static int sm_pair(long N, long cols, long I, bool half, const SmPlan &dx, const
 }
 static int low_groups(size_t rows) { return rows >= 4096 ? (int)((rows + 3) / 4) : (int)rows; }
 
+// Few fp32 rows go by the weights as they lie (smfew.hpp): as planes these are read, written and read again.  us here and as planes, outputs and their statistics,
+// then gradients: 1 x 2048 -> 65536 111 / 346 and 368 / 777, 48 x 1024 -> 65536 104 / 172 and 315 / 402, 12 x 2048 -> 1000 16 / 18 and 25 / 36, 64 x 1024 -> 65536 122 / 176
+// and 350 / 405.  A work-group walks all of k, so that long rows of few classes leave most of the chip idle (48 x 8192 -> 2048: 71 / 53 and 123 / 105), and the
+// gradients of more than 48 rows take the matrix unit's time where there are few classes, too (64 x 1024 -> 1000: 36 / 32).
+constexpr int kSmFewRows = 64, kSmFew = SM_TILES;
+static bool sm_few(bool half, bool forward, int N, int I, int ol)
+{
+    if (!half || N < 1 || N > kSmFewRows) return false;
+    const int want = forced_tile() - kSmFirstTile;
+    if (want >= 0 && want <= kSmFew) return want == kSmFew;
+    return forced_split() <= 0 && (ol >= 4096 || (I <= 2048 && (forward || N <= 48)));
+}
+
 // Scratch of a pass, laid out in order.
 struct SmLayout {
+    bool few;                   // few fp32 rows
+    int strip;                  // classes of a work-group of their backward pass
     bool half, laid;            // fp32; w is laid out
     int isteps, piece, pieces;  // steps of memory of a row of x or w; classes of a piece, pieces
     int products;               // of outputs and of dx, per step of memory
@@ -407,6 +423,31 @@ struct SmLayout {
         isteps = up(I, 64);
         laid = half || I % 64;
         products = half ? SM_THREE : SM_ONE;
+        few = sm_few(half, forward, N, I, ol);
+        if (few) {
+            size_t at = 0;
+            auto take = [&](size_t bytes) { const size_t was = at; at += (bytes + 255) / 256 * 256; return was; };
+            x = w = xexp = wexp = xlows = wlows = least = top = label_out = dz = dz_dx = dxs = strips = partial = 0;
+            piece = ol;
+            pieces = 1;
+            z = dx = dw = {SM_BIG, 1, 0.f};
+            pair = SM_NOTHING;
+            // of 256 columns: as many strips of classes as fill the chip at its registers' two or four work-groups a CU, unless their parts of dx grow beyond w itself
+            const int across = up(I, 256), most = up(ol, 16), rows = up(N, 16);
+            auto strip_of = [&](int groups) { return up(most, most < up(groups, across) ? most : up(groups, across)); };
+            strip = strip_of(rows > 2 ? 512 : 1024);
+            if (strip < rows) strip = rows < strip_of(256) ? rows : strip_of(256);
+            strip *= 16;
+            if (forward) {
+                top = take((size_t)up(ol, 16 * few_blocks(N, ol)) * few_blocks(N, ol) * N * sizeof(Top));
+                label_out = take((size_t)N * 4);
+            } else {
+                dz = take((size_t)N * few_pitch(ol) * 4);
+                partial = take((size_t)up(ol, strip) * N * I * 4);
+            }
+            total = at;
+            return;
+        }
         const size_t row = (size_t)isteps * (half ? 256 : 128);
         auto plans = [&](int cols) {
             piece = cols;
@@ -472,6 +513,10 @@ struct SmLayout {
         partial = take(parts);
         total = N ? at : 0;
     }
+    // Blocks of 16 classes of a work-group of the outputs: more of them read x less often, fewer fill the chip (us with 1, 2, 4: 1 x 2048 -> 65536 99, 130, 112,
+    // 32 x 2048 -> 8192 26, 24, 31, 48 x 2048 -> 16384 61, 48, 43).  dz's rows.
+    static int few_blocks(int N, int ol) { return N <= 16 || ol < 8192 ? 1 : ol < 16384 ? 2 : 4; }
+    static int few_pitch(int ol) { return up(ol, 64) * 64; }
     bool fits() const { return z.tile >= 0 && dx.tile >= 0 && dw.tile >= 0; }
     // Classes of a piece: as many as `fit`, but pieces alike
     static int alike(size_t fit, size_t least, int ol, int more = 0)
@@ -637,12 +682,70 @@ static SmParams outputs(const owt_fc_desc *d, const SmLayout &l, char *ws, const
     return p;
 }
 
+// What the passes over few rows have in common, and their launches by blocks of 16 rows
+static SmFewParams few_params(const owt_fc_desc *d, const SmLayout &l, int ol, const void *x, const void *w, const float *bias, const int *labels, char *ws)
+{
+    SmFewParams f;
+    memset(&f, 0, sizeof(f));
+    f.x = (const float *)x;
+    f.w = (const float *)w;
+    f.I = d->I;
+    f.dz = (float *)(ws + l.dz);
+    f.pitch = SmLayout::few_pitch(ol);
+    f.p.M = d->N;
+    f.p.N = ol;
+    f.p.bias = bias;
+    f.p.labels = labels;
+    f.p.classes = d->O_total;
+    f.p.off = d->rank * ol;
+    f.strip = l.strip;
+    f.strips = up(ol, l.strip);
+    return f;
+}
+template <int NB, bool DZ> static void few_outputs(const SmFewParams &f, hipStream_t s)
+{
+    const int blocks = SmLayout::few_blocks(f.p.M, f.p.N);
+    const dim3 grid((unsigned)up(f.p.N, 16 * blocks));
+    if constexpr (NB > 1) {
+        if (blocks == 4) { hipLaunchKernelGGL((sm_few_kernel<NB, 4, DZ>), grid, dim3(256), 0, s, f); return; }
+        if (blocks == 2) { hipLaunchKernelGGL((sm_few_kernel<NB, 2, DZ>), grid, dim3(256), 0, s, f); return; }
+    }
+    hipLaunchKernelGGL((sm_few_kernel<NB, 1, DZ>), grid, dim3(256), 0, s, f);
+}
+template <bool DZ> static void few_outputs(const SmFewParams &f, hipStream_t s)
+{
+    switch (up(f.p.M, 16)) {
+    case 1: return few_outputs<1, DZ>(f, s);
+    case 2: return few_outputs<2, DZ>(f, s);
+    case 3: return few_outputs<3, DZ>(f, s);
+    default: return few_outputs<4, DZ>(f, s);
+    }
+}
+static void few_gradients(const SmFewParams &f, hipStream_t s)
+{
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)up(f.I, 256), (unsigned)f.strips), dim3(256), 0, s, f); };
+    switch (up(f.p.M, 16)) {
+    case 1: return go(sm_few_back_kernel<1>);
+    case 2: return go(sm_few_back_kernel<2>);
+    case 3: return go(sm_few_back_kernel<3>);
+    default: return go(sm_few_back_kernel<4>);
+    }
+}
+
 static owt_status forward(const owt_fc_desc *d, const SmLayout &l, int ol, const void *x, const void *w, const float *bias, const int *labels, float *lse, float *target,
                           float *loss, char *ws, hipStream_t s)
 {
     const SmSource from{d, l, ws, s};
     SmRows r = {(const Top *)(ws + l.top), 0, d->N, (const float *)(ws + l.label_out), labels, d->O_total, d->rank * ol, ol, lse, target, loss};
-    for (int k = 0; k < l.pieces; k++) {
+    if (l.few) {
+        SmFewParams f = few_params(d, l, ol, x, w, bias, labels, ws);
+        f.p.top = (Top *)(ws + l.top);
+        f.p.target = (float *)(ws + l.label_out);
+        few_outputs<false>(f, s);
+        const int blocks = SmLayout::few_blocks(d->N, ol);
+        r.parts = up(ol, 16 * blocks) * blocks;
+    }
+    for (int k = 0; k < (l.few ? 0 : l.pieces); k++) {
         const int v0 = k * l.piece, cols = ol - v0 < l.piece ? ol - v0 : l.piece;
         SmOperand xo, wo;
         from.operands(x, w, k, v0, cols, nullptr, nullptr, true, xo, wo);
@@ -681,6 +784,24 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
             none.N = 1;
             none.out = db;
             join_parts(false, none, s);
+        }
+        return launched();
+    }
+    if (l.few) {
+        SmFewParams f = few_params(d, l, ol, x, w, bias, labels, ws);
+        f.p.lse = lse;
+        f.p.weight = weight;
+        few_outputs<true>(f, s);
+        f.p.alpha = alpha;
+        f.p.beta = beta;
+        f.p.out = dw;
+        f.p.db = db;
+        f.p.big = (size_t)ol * d->I * 4 > (32u << 20) && d->I % 32 == 0;
+        f.p.partial = dx ? (float *)(ws + l.partial) : nullptr;
+        few_gradients(f, s);
+        if (dx) {
+            f.p.out = dx;
+            hipLaunchKernelGGL(sm_few_join_kernel, dim3((unsigned)up((size_t)d->N * d->I, 256)), dim3(1024), 0, s, f);
         }
         return launched();
     }

@@ -345,6 +345,34 @@ def test_tiles_and_splits(N, I, O, tile, splits, dt):
         assert_within(got[k], want, off, k)
 
 
+FEW = 124              # few rows of fp32 with the weights as they lie
+
+
+@pytest.mark.parametrize("N,I,O", [(1, 1, 1), (1, 1300, 70), (3, 5, 65), (16, 130, 257), (17, 33, 1000), (32, 256, 64), (40, 64, 300), (64, 259, 130), (48, 512, 1030),
+                                   (5, 64, 16401), (20, 36, 17000), (64, 31, 16500), (33, 40, 9000), (60, 100, 8200)])
+def test_few_rows(N, I, O):
+    from gpu_util import force
+    with force(FEW, 0):
+        test_forward(N, I, O, "f32")
+        test_backward(N, I, O, "f32")
+
+
+def test_few_rows_with_all_that_may_be_in_them():
+    from gpu_util import force
+    with force(FEW, 0):
+        for N, I, O in ((5, 40, 70), (40, 2048, 96), (64, 68, 520)):
+            test_rows_without_a_class_have_no_influence(N, I, O, "f32")
+            test_classes_that_are_taken_out(N, I, O, "f32")
+            test_the_same_call_gives_the_same_bits_and_writes_its_results_alone(N, I, O, "f32")
+        test_captured_and_replayed(16, 128, 2000, "f32")
+
+
+@pytest.mark.parametrize("N,I,O", [(1, 2048, 4100), (16, 1024, 17000), (64, 1030, 5001)])
+def test_few_rows_of_large_layers(N, I, O):
+    test_forward(N, I, O, "f32")
+    test_backward(N, I, O, "f32")
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_pieces(dt):
     """So many rows that the classes are taken in pieces, the last of them short; few values of x, so that the reference is quick."""
