@@ -393,8 +393,8 @@ static int sm_pair(long N, long cols, long I, bool half, const SmPlan &dx, const
 static int low_groups(size_t rows) { return rows >= 4096 ? (int)((rows + 3) / 4) : (int)rows; }
 
 // Few fp32 rows go by the weights as they lie (smfew.hpp): as planes these are read, written and read again.  us here and as planes, outputs and their statistics,
-// then gradients: 1 x 2048 -> 65536 111 / 346 and 368 / 777, 48 x 1024 -> 65536 104 / 172 and 315 / 402, 12 x 2048 -> 1000 16 / 18 and 25 / 36, 64 x 1024 -> 65536 122 / 176
-// and 350 / 405.  A work-group walks all of k, so that long rows of few classes leave most of the chip idle (48 x 8192 -> 2048: 71 / 53 and 123 / 105), and the
+// then gradients: 1 x 2048 -> 65536 111 / 346 and 368 / 777, 48 x 1024 -> 65536 101 / 172 and 307 / 402, 12 x 2048 -> 1000 16 / 18 and 25 / 36, 64 x 1024 -> 65536 112 / 176
+// and 345 / 405.  A work-group walks all of k, so that long rows of few classes leave most of the chip idle (48 x 8192 -> 2048: 71 / 53 and 123 / 105), and the
 // gradients of more than 48 rows take the matrix unit's time where there are few classes, too (64 x 1024 -> 1000: 36 / 32).
 constexpr int kSmFewRows = 64, kSmFew = SM_TILES;
 static bool sm_few(bool half, bool forward, int N, int I, int ol)
