@@ -364,9 +364,9 @@ static size_t partial_bytes(const SmPlan &pl, long M, long N) { return pl.splits
 static int strips_of(const SmPlan &z, int N) { return z.splits > 1 ? up(N, 32) : up(N, kSmTiles[z.tile].bm) * kSmTiles[z.tile].wm; }
 
 // Both backward products in one launch, dx's sums perhaps split: worth its tile where neither fills the chip for long.  Returns the tile or SM_NOTHING, the plan of dx in x.
-static int sm_pair(long N, long cols, long I, bool half, const SmPlan &dx, const SmPlan &dw, SmPlan &x)
+static int sm_pair(long N, long cols, long I, int products_x, int products_w, const SmPlan &dx, const SmPlan &dw, SmPlan &x)
 {
-    const int want = forced_tile() - kSmFirstTile, products_x = half ? SM_THREE : SM_ONE, products_w = half ? SM_THREE : SM_PAIR;
+    const int want = forced_tile() - kSmFirstTile;
     const int most = up((int)cols, 64), steps_w = up((int)N, 64) * products_w;
     if (forced_split() > 0) return SM_NOTHING;
     float least = want >= 0 && want < SM_TILES ? 1e30f : dx.us + dw.us;
@@ -405,13 +405,20 @@ static bool sm_few(bool half, bool forward, int N, int I, int ol)
     return forced_split() <= 0 && (ol >= 4096 || (I <= 2048 && (forward || N <= 48)));
 }
 
+// bf16 layers of up to so many products, where launches are most of what it costs: dz in three bf16 values for dw, all its 24 bits, and in two for dx.  dw of 15 x 192
+// -> 512 is off by 5.4e-7 of its size then (2.2e-6 with two), dx by its own rounding's 0.0017 (0.0020); us: 15 x 384 -> 10 11.7 (11.6), 707 x 1024 -> 36 27.5 (21.8),
+// 128 x 4096 -> 512 25.6 (23.6), 1000 x 1000 -> 250 37.8 (29.9).  A quarter of the time of a large layer would be for what its outputs' own sums lose.
+constexpr double kSmLittle = (double)((size_t)1 << 28);
+
 // Scratch of a pass, laid out in order.
 struct SmLayout {
     bool few;                   // few fp32 rows
     int strip;                  // classes of a work-group of their backward pass
     bool half, laid;            // fp32; w is laid out
     int isteps, piece, pieces;  // steps of memory of a row of x or w; classes of a piece, pieces
-    int products;               // of outputs and of dx, per step of memory
+    int products;               // of outputs, per step of memory
+    int products_x, products_w; // of dx and of dw
+    int planes;                 // of dz
     SmPlan z, dx, dw;           // of a whole piece
     int pair;                   // the tile of dx and dw in one launch, or nothing
     SmPlan together;            // dx's part of it
@@ -423,6 +430,10 @@ struct SmLayout {
         isteps = up(I, 64);
         laid = half || I % 64;
         products = half ? SM_THREE : SM_ONE;
+        const bool little = !half && (double)N * I * ol <= kSmLittle;
+        products_x = half ? SM_THREE : little ? SM_PAIR : SM_ONE;
+        products_w = half || little ? SM_THREE : SM_PAIR;
+        planes = little ? 3 : 2;
         few = sm_few(half, forward, N, I, ol);
         if (few) {
             size_t at = 0;
@@ -454,8 +465,8 @@ struct SmLayout {
             pieces = up(ol, cols);
             z = sm_plan(N, cols, isteps * products, products, forward ? SM_TOP : SM_DZ);
             if (forward) return;
-            dx = sm_plan(N, I, up(cols, 64) * products, products, SM_OUT);
-            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * (half ? SM_THREE : SM_PAIR), half ? SM_THREE : SM_PAIR, SM_OUT);
+            dx = sm_plan(N, I, up(cols, 64) * products_x, products_x, SM_OUT);
+            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * products_w, products_w, SM_OUT);
         };
         auto us = [&] { return (float)pieces * (z.us + dx.us + dw.us); };
         if (forward) plans(forward_piece(laid, row, ol));
@@ -497,11 +508,11 @@ struct SmLayout {
             label_out = take((size_t)N * 4);
         } else {
             const int psteps = up(piece, 64);
-            dz = take((size_t)N * psteps * 256);
+            dz = take((size_t)N * psteps * 128 * planes);
             dz_dx = take(half ? (size_t)N * psteps * 256 : 0);
             dxs = take(!half && pieces > 1 ? (size_t)N * I * 4 : 0);
             strips = take((size_t)strips_of(z, N) * piece * 4);
-            pair = sm_pair(N, piece, I, half, dx, dw, together);
+            pair = sm_pair(N, piece, I, products_x, products_w, dx, dw, together);
             if (pair != SM_NOTHING) {
                 dx = together;
                 dw = {pair, 1, 0.f};
@@ -806,7 +817,7 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
         return launched();
     }
     const SmSource from{d, l, ws, s};
-    const int products = l.half ? SM_THREE : SM_PAIR, nsteps = up(d->N, 64);
+    const int nsteps = up(d->N, 64), step = 128 * l.planes;
     int *least = (int *)(ws + l.least);
     for (int k = 0; k < l.pieces; k++) {
         const int v0 = k * l.piece, cols = ol - v0 < l.piece ? ol - v0 : l.piece, psteps = up(cols, 64);
@@ -817,7 +828,8 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
         p.weight = weight;
         p.dz = (unsigned char *)(ws + l.dz);
         p.dz_dx = (unsigned char *)(ws + l.dz_dx);
-        p.dz_ld = (size_t)psteps * 256;
+        p.dz_ld = (size_t)psteps * step;
+        p.dz_step = step;
         p.lows_x = (const int *)(ws + l.xlows);
         p.lows_w = (const int *)(ws + l.wlows);
         p.num_x = low_groups(up(d->N, 64) * 64);
@@ -836,11 +848,11 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
         SmParams qx = none;
         if (dx) {
             SmParams &q = qx;
-            q.a = {l.half ? p.dz_dx : p.dz, p.dz_ld, 256, d->N, 0, 2};
+            q.a = {l.half ? p.dz_dx : p.dz, p.dz_ld, (size_t)step, d->N, 0, l.planes};
             q.b = SmSource::across(wo, cols, l.isteps);
             q.M = d->N;
             q.N = d->I;
-            q.products = l.half ? SM_THREE : SM_ONE;
+            q.products = l.products_x;
             q.steps = psteps * q.products;
             q.labels = labels;
             q.classes = d->O_total;
@@ -856,12 +868,12 @@ static owt_status backward(const owt_fc_desc *d, const SmLayout &l, int ol, cons
             lay_tiles(q, l.dx);
         }
         SmParams q = none;
-        q.a = {p.dz, p.dz_ld, 64 * p.dz_ld, d->N, 8 * psteps, 2};
+        q.a = {p.dz, p.dz_ld, 64 * p.dz_ld, d->N, 8 * psteps, l.planes};
         q.b = SmSource::across(from.along(ws + l.x, d->N), nsteps * 64, l.isteps);
         q.M = cols;
         q.N = d->I;
-        q.products = products;
-        q.steps = nsteps * products;
+        q.products = l.products_w;
+        q.steps = nsteps * l.products_w;
         q.alpha = alpha;
         q.beta = beta;
         q.under = least;

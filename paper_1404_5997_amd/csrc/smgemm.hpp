@@ -73,7 +73,8 @@ struct SmOperand {
     int planes;
 };
 
-enum { SM_ONE = 1, SM_PAIR = 2, SM_THREE = 3 };     // products of a step of memory: one; both planes of A with B; the three larger of both planes of both
+// products of a step of memory: one; two planes of A with B; three planes of A with B, or where A has two the three larger of both planes of both
+enum { SM_ONE = 1, SM_PAIR = 2, SM_THREE = 3 };
 
 // Rows of x or w laid out for the products: whole steps of 64 values, zeros behind the last one, and zeros for rows without a class (labels null: all have one).
 struct SmPrep {
@@ -104,6 +105,7 @@ struct SmParams {
     const float *lse, *weight;
     unsigned char *dz, *dz_dx;
     size_t dz_ld;
+    int dz_step;            // bytes of 64 classes: 128 a plane
     const int *lows_x, *lows_w; // what the least exponents are the least of
     int num_x, num_w;
     int *least;                 // [0] of x, [1] of w: for the products that follow
@@ -212,14 +214,18 @@ __device__ __forceinline__ void sm_put_halves(unsigned char *to, const float (&v
     *(uint2 *)to = make_uint2(sm_halves(v[0], v[1]), sm_halves(v[2], v[3]));
     *(uint2 *)(to + 128) = make_uint2(sm_halves(lo[0], lo[1]), sm_halves(lo[2], lo[3]));
 }
-// and as two bf16 ones
-__device__ __forceinline__ void sm_put_bf16s(unsigned char *to, const float (&v)[4])
+// and as two bf16 ones, or three
+__device__ __forceinline__ void sm_put_bf16s(unsigned char *to, const float (&v)[4], bool three)
 {
     const uint2 hi = make_uint2(f32x2_to_bf16x2(v[0], v[1]), f32x2_to_bf16x2(v[2], v[3]));
     const float lo[4] = {v[0] - __uint_as_float(hi.x << 16), v[1] - __uint_as_float(hi.x & 0xffff0000u), v[2] - __uint_as_float(hi.y << 16),
                          v[3] - __uint_as_float(hi.y & 0xffff0000u)};
     *(uint2 *)to = hi;
-    *(uint2 *)(to + 128) = make_uint2(f32x2_to_bf16x2(lo[0], lo[1]), f32x2_to_bf16x2(lo[2], lo[3]));
+    const uint2 second = make_uint2(f32x2_to_bf16x2(lo[0], lo[1]), f32x2_to_bf16x2(lo[2], lo[3]));
+    *(uint2 *)(to + 128) = second;
+    if (three)
+        *(uint2 *)(to + 256) = make_uint2(f32x2_to_bf16x2(lo[0] - __uint_as_float(second.x << 16), lo[1] - __uint_as_float(second.x & 0xffff0000u)),
+                                          f32x2_to_bf16x2(lo[2] - __uint_as_float(second.y << 16), lo[3] - __uint_as_float(second.y & 0xffff0000u)));
 }
 // The least exponents of x's rows with their weights and of w's, found by the work-group for itself; `first` leaves them to the products that follow.
 // two: eight words of LDS that nothing else is in.
@@ -266,7 +272,7 @@ __device__ __forceinline__ void sm_dz(const SmParams &p, int2 least, int m, int 
         sums[t] += d[t];
     }
     if (m >= p.M || c >= (p.N + 63) / 64 * 64) return;
-    const size_t at = (size_t)m * p.dz_ld + (size_t)(c >> 6) * 256 + 2 * (c & 63);
+    const size_t at = (size_t)m * p.dz_ld + (size_t)(c >> 6) * (SCALED ? 256 : p.dz_step) + 2 * (c & 63);
     if (SCALED) {
         const int ex = kSmDzTop - (w.exp - least.x), lw = least.y + kSmDzTop;
 #pragma unroll
@@ -276,7 +282,7 @@ __device__ __forceinline__ void sm_dz(const SmParams &p, int2 least, int m, int 
         }
         sm_put_halves(p.dz + at, d);
         sm_put_halves(p.dz_dx + at, e);
-    } else sm_put_bf16s(p.dz + at, d);
+    } else sm_put_bf16s(p.dz + at, d, p.dz_step == 384);
 }
 
 struct __attribute__((packed, aligned(2))) SmFourHalves { uint32_t lo, hi; };
@@ -332,8 +338,9 @@ __device__ __forceinline__ void sm_tile(const SmParams &p, int tile, int split, 
             pa = s & 1;
         } else if (p.products == SM_THREE) {
             t = s / 3;
-            pa = s - 3 * t == 2;
-            pb = s - 3 * t == 1;
+            const int i = s - 3 * t;
+            pa = p.a.planes == 3 ? i : i == 2;
+            pb = p.a.planes == 3 ? 0 : i == 1;
         }
         // the last rows of k: what is loaded behind them is the same step's
         if (TA && 64 * t + 64 > p.a.rows) {

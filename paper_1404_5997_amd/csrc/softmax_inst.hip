@@ -23,7 +23,7 @@ template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmP
         if (ring) return go<TA, TB, SmBigThree, END>(p, s);
 #else
         if constexpr (TA)
-            if (ring) return go<TA, TB, SmBigPair, END>(p, s);
+            if (ring && p.products == SM_PAIR) return go<TA, TB, SmBigPair, END>(p, s);
 #endif
         return go<TA, TB, SmBig, END>(p, s);
     }

@@ -75,13 +75,15 @@ class Reference:
         return d * f, off * np.abs(f)
 
 
-def grads(ref, lse, weight, dt, alpha, beta, dw0, db0):
-    """(dx, dw, db) and the bounds of their errors."""
+def grads(ref, lse, weight, dt, alpha, beta, dw0, db0, little=False):
+    """(dx, dw, db) and the bounds of their errors; little: of a small bf16 layer, dz in three values for dw (each rounding leaves 2^-8, the third 2^-24) and in two for dx."""
     dz, off = ref.dz(lse, weight)
     N, O = dz.shape
     second = planes_error(dt)
     aw, ax = np.abs(ref.w), np.abs(ref.x)
     one = 2.0 ** -8 if dt == "bf16" else second
+    if little:
+        second, one = 2.0 ** -24, 2.0 ** -16
     # dz in two f16 values is at 2^15 for 1 under one power of two: off by 2^-25 under it, 2^-40 without.  For dw a row n of dz comes times 2^-e, e of x's row, times the weight,
     # and the power of two is the largest such factor's or up to twice that; 2^-e is x's largest magnitude over 2^14 .. 2^15: the row's 2^-40 is that times the largest row's
     # weight times magnitude over this row's magnitude, times 4.  For dx the same with w's rows and no weight.  x and w have floors of their own.

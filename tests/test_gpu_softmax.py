@@ -345,6 +345,26 @@ def test_tiles_and_splits(N, I, O, tile, splits, dt):
         assert_within(got[k], want, off, k)
 
 
+@pytest.mark.parametrize("splits", [0, 1, 3])
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("N,I,O", [(520, 640, 1030), (1100, 512, 600), (130, 2100, 1000)])
+def test_tiles_and_splits_of_larger_layers(N, I, O, tile, splits):
+    test_tiles_and_splits(N, I, O, tile, splits, "bf16")
+
+
+@pytest.mark.parametrize("tile", ["planned"] + list(TILES))
+@pytest.mark.parametrize("N,I,O", [(1, 1, 1), (15, 384, 10), (65, 63, 129), (300, 130, 70), (128, 256, 1000), (900, 64, 300)])
+def test_small_layers_keep_all_of_dz(N, I, O, tile):
+    from gpu_util import force
+    x, w, b, labels, weight = inputs(N, I, O, N + O + 2, "bf16")
+    ref = Reference(x, w, b, labels)
+    lse = ref.lse.astype(np.float32)
+    with force(TILES.get(tile, -1), 0):
+        got = run_bwd(N, I, O, "bf16", x, w, b, labels, lse, weight, 1.0 / N, 0.0, None, None)
+    for k, (want, off) in grads(ref, lse, weight, "bf16", 1.0 / N, 0.0, None, None, little=True).items():
+        assert_within(got[k], want, off, k)
+
+
 FEW = 124              # few rows of fp32 with the weights as they lie
 
 
