@@ -352,6 +352,18 @@ def test_tiles_and_splits_of_larger_layers(N, I, O, tile, splits):
     test_tiles_and_splits(N, I, O, tile, splits, "bf16")
 
 
+@pytest.mark.parametrize("N,I,O", [(1, 2048, 8300), (64, 300, 15000), (17, 4100, 4104)])
+def test_dw_of_few_rows_keeps_all_of_dz(N, I, O):
+    x, w, b, labels, weight = inputs(N, I, O, N + O + 3, "bf16")
+    ref = Reference(x, w, b, labels)
+    lse = ref.lse.astype(np.float32)
+    got = run_bwd(N, I, O, "bf16", x, w, b, labels, lse, weight, 1.0 / N, 0.0, None, None)
+    want = grads(ref, lse, weight, "bf16", 1.0 / N, 0.0, None, None)
+    want["dw"] = grads(ref, lse, weight, "bf16", 1.0 / N, 0.0, None, None, little=True)["dw"]
+    for k in want:
+        assert_within(got[k], *want[k], k)
+
+
 @pytest.mark.parametrize("tile", ["planned"] + list(TILES))
 @pytest.mark.parametrize("N,I,O", [(1, 1, 1), (15, 384, 10), (65, 63, 129), (300, 130, 70), (128, 256, 1000), (900, 64, 300)])
 def test_small_layers_keep_all_of_dz(N, I, O, tile):
