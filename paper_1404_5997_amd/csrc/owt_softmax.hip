@@ -408,7 +408,7 @@ static bool sm_few(bool half, bool forward, int N, int I, int ol)
 // bf16 layers of up to so many products, and a sixteenth as many weights, where launches are most of what it costs: dz in three bf16 values for dw, all its 24 bits, and in two for dx.  dw of 15 x 192
 // -> 512 is off by 5.4e-7 of its size then (2.2e-6 with two), dx by its own rounding's 0.0017 (0.0020); us: 15 x 384 -> 10 11.7 (11.6), 707 x 1024 -> 36 27.5 (21.8),
 // 128 x 4096 -> 512 25.6 (23.6), 1000 x 1000 -> 250 37.8 (29.9).  Rows of one step, up to 64,
-// take three for dw, too, whose sums are too short to lose as much themselves: 16 x 2048 -> 65536 234 us (211).  A quarter of the time of larger layers would be for what their
+// take three for dw, too, whose sums are too short to lose as much themselves: 16 x 2048 -> 65536 225 us (211).  A quarter of the time of larger layers would be for what their
 // outputs' own sums lose.
 constexpr double kSmLittle = (double)((size_t)1 << 28);
 constexpr int kSmFewOfAll = 64;
@@ -469,7 +469,9 @@ struct SmLayout {
             z = sm_plan(N, cols, isteps * products, products, forward ? SM_TOP : SM_DZ);
             if (forward) return;
             dx = sm_plan(N, I, up(cols, 64) * products_x, products_x, SM_OUT);
-            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * products_w, products_w, SM_OUT);
+            // (few rows of many weights: the third product is behind the results' writing, 16 x 2048 -> 65536 148 us, 161 where the tile is chosen for it)
+            const int shown = planes == 3 && (double)I * ol > kSmLittle / 16 ? SM_PAIR : products_w;
+            dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * shown, shown, SM_OUT);
         };
         auto us = [&] { return (float)pieces * (z.us + dx.us + dw.us); };
         if (forward) plans(forward_piece(laid, row, ol));
