@@ -332,9 +332,9 @@ size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass);     /* (
  * N, I, O_local <= 2^22, x and w of at most 2^31-1 values, no more tiles of outputs than a launch counts (OWT_EUNSUPPORTED).
  *
  * bf16 operands are multiplied as they are.  fp32 ones may be multiplied as sums of two f16 values under a power of two for each row of x and of w,
- * which hold 22 bits of all that is within 2^-16 of the row's largest magnitude, and 2^-39 of the largest below that.  dz meets x, for dw, as the sum of
- * two bf16 values (16 bits) or of two f16 ones, and w, for dx, as one bf16 value (dx is rounded to bf16 itself) or as two f16 ones; bf16 of up to
- * N I O_local = 2^28 and I O_local = 2^24 takes three (24 bits) and two, other bf16 of up to 64 rows three for dw.  f16 values of dz are under
+ * which hold 22 bits of all that is within 2^-16 of the row's largest magnitude, and 2^-39 of the largest below that.  dz is the sum of two bf16
+ * values (16 bits) or of two f16 ones, whatever dx is stored in; for dw it is the sum of three bf16 values (24 bits) where N I O_local <= 2^28 and
+ * I O_local <= 2^24, or N <= 64.  f16 values of dz are under
  * one power of two for all rows: of exp(z - lse) and of 1 they hold 22 bits down to 2^-18, and 2^-40 below that (where rows of x, with their weights, or
  * of w differ in size, times the ratio of the largest row's largest magnitude to that of the row that is met, and up to four). */
 

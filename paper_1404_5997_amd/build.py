@@ -44,6 +44,7 @@ def _units():
     for half, hname in ((0, "bf16"), (1, "half")):
         for out, oname in ((0, "ends"), (1, "out")):
             units.append(("softmax_%s_%s.o" % (hname, oname), "softmax_inst.hip", ["-DOWT_INST_HALF=%d" % half, "-DOWT_INST_OUT=%d" % out]))
+    units.append(("softmax_bf16_dx.o", "softmax_inst.hip", ["-DOWT_INST_HALF=0", "-DOWT_INST_OUT=2"]))
     units.append(("xfilter.o", "xfilter_inst.hip", []))
     units.append(("xgather.o", "xgather_inst.hip", []))
     for masked in (0, 1):

@@ -405,11 +405,12 @@ static bool sm_few(bool half, bool forward, int N, int I, int ol)
     return forced_split() <= 0 && (ol >= 4096 || (I <= 2048 && (forward || N <= 48)));
 }
 
-// bf16 layers of up to so many products, and a sixteenth as many weights, where launches are most of what it costs: dz in three bf16 values for dw, all its 24 bits, and in two for dx.  dw of 15 x 192
-// -> 512 is off by 5.4e-7 of its size then (2.2e-6 with two), dx by its own rounding's 0.0017 (0.0020); us: 15 x 384 -> 10 11.7 (11.6), 707 x 1024 -> 36 27.5 (21.8),
-// 128 x 4096 -> 512 25.6 (23.6), 1000 x 1000 -> 250 37.8 (29.9).  Rows of one step, up to 64,
-// take three for dw, too, whose sums are too short to lose as much themselves: 16 x 2048 -> 65536 225 us (211).  A quarter of the time of larger layers would be for what their
-// outputs' own sums lose.
+// dx takes dz in two bf16 values, 16 bits of it, in every bf16 layer.  A row's dz add up to zero, so that what all classes' weights have in common cancels in dx, and what one value
+// loses, 2^-9 of each term, does not: where the weights differ by a 32nd of their size one value left dx off by 40 to 70 times what its sums and its own rounding explain.
+// us with two (one): 16 x 2048 -> 65536 284 (247), 777 x 1537 -> 20011 363 (321), 4096 x 4096 -> 65536 8450 (7090).
+// dw takes it in three, all its 24 bits, in bf16 layers of up to so many products, and a sixteenth as many weights, where launches are most of what it costs: dw of 15 x 192
+// -> 512 is off by 5.4e-7 of its size then (2.2e-6 with two).  Rows of one step, up to 64, take three, too, as their sums are too short to lose as much themselves.  A quarter of the
+// time of larger layers would be for what their outputs' own sums lose.
 constexpr double kSmLittle = (double)((size_t)1 << 28);
 constexpr int kSmFewOfAll = 64;
 
@@ -434,7 +435,7 @@ struct SmLayout {
         laid = half || I % 64;
         products = half ? SM_THREE : SM_ONE;
         const bool little = !half && (double)N * I * ol <= kSmLittle && (double)I * ol <= kSmLittle / 16;
-        products_x = half ? SM_THREE : little ? SM_PAIR : SM_ONE;
+        products_x = half ? SM_THREE : SM_PAIR;
         products_w = half || little || N <= kSmFewOfAll ? SM_THREE : SM_PAIR;
         planes = !half && products_w == SM_THREE ? 3 : 2;
         few = sm_few(half, forward, N, I, ol);

@@ -22,6 +22,7 @@ enum { SM_PRODUCT_TOP, SM_PRODUCT_DZ, SM_PRODUCT_Z, SM_PRODUCT_DX, SM_PRODUCT_DW
 // half: fp32 values as two f16 ones; else bf16
 hipError_t owt_launch_softmax_bf16_ends(int product, int tile, const SmParams &, hipStream_t);      // TOP, DZ
 hipError_t owt_launch_softmax_bf16_out(int product, int tile, const SmParams &, hipStream_t);       // Z, DX, DW
+hipError_t owt_launch_softmax_bf16_dx(const SmParams &, hipStream_t);       // DX, long sums of two products in 256 x 256 tiles
 hipError_t owt_launch_softmax_half_ends(int product, int tile, const SmParams &, hipStream_t);
 hipError_t owt_launch_softmax_half_out(int product, int tile, const SmParams &, hipStream_t);
 // dx and dw together: 128 x 128 or 64 x 64

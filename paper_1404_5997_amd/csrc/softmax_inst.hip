@@ -1,4 +1,5 @@
-// Instantiations of smgemm.hpp: -DOWT_INST_HALF=0 (bf16) or 1 (f16), -DOWT_INST_OUT=0 (outputs as statistics or dz) or 1 (stored sums).
+// Instantiations of smgemm.hpp: -DOWT_INST_HALF=0 (bf16) or 1 (f16), -DOWT_INST_OUT=0 (outputs as statistics or dz), 1 (stored sums) or
+// 2 (bf16 dx of long sums in 256 x 256 tiles).
 #include "softmax.hpp"
 
 namespace owt {
@@ -15,6 +16,10 @@ template <bool TA, bool TB, class S, int END> static hipError_t go(const SmParam
                        s, p);
     return hipGetLastError();
 }
+#if OWT_INST_OUT == 2
+hipError_t owt_launch_softmax_bf16_dx(const SmParams &p, hipStream_t s) { return go<false, true, SmBigPair, SM_OUT>(p, s); }
+#else
+
 template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmParams &p, hipStream_t s)
 {
     if (tile == SM_BIG) {
@@ -22,8 +27,11 @@ template <bool TA, bool TB, int END> static hipError_t tiled(int tile, const SmP
 #if OWT_INST_HALF
         if (ring) return go<TA, TB, SmBigThree, END>(p, s);
 #else
-        if constexpr (TA)
-            if (ring && p.products == SM_PAIR) return go<TA, TB, SmBigPair, END>(p, s);
+        if constexpr (TB)
+            if (ring && p.products == SM_PAIR) {
+                if constexpr (TA) return go<TA, TB, SmBigPair, END>(p, s);
+                else return owt_launch_softmax_bf16_dx(p, s);
+            }
 #endif
         return go<TA, TB, SmBig, END>(p, s);
     }
@@ -69,6 +77,7 @@ hipError_t owt_launch_softmax_bf16_pair(int tile, const SmParams &x, const SmPar
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }
+#endif
 #endif
 
 }  // namespace owt
