@@ -391,6 +391,8 @@ static int sm_pair(long N, long cols, long I, int products_x, int products_w, co
     return best;
 }
 static int low_groups(size_t rows) { return rows >= 4096 ? (int)((rows + 3) / 4) : (int)rows; }
+// of `rows` rows or fewer: 4095, one by one, are more work-groups than 4096 by fours
+static int most_low_groups(size_t rows) { return rows >= 4096 && low_groups(rows) < 4095 ? 4095 : low_groups(rows); }
 
 // Few fp32 rows go by the weights as they lie (smfew.hpp): as planes these are read, written and read again.  us here and as planes, outputs and their statistics,
 // then gradients: 1 x 2048 -> 65536 111 / 346 and 368 / 777, 48 x 1024 -> 65536 101 / 172 and 307 / 402, 12 x 2048 -> 1000 16 / 18 and 25 / 36, 64 x 1024 -> 65536 112 / 176
@@ -502,7 +504,7 @@ struct SmLayout {
         xexp = take(half ? (size_t)N * 4 : 0);
         wexp = take(half ? (size_t)piece * 4 : 0);
         xlows = take(half && !forward ? (size_t)low_groups(rows) * 4 : 0);
-        wlows = take(half && !forward ? (size_t)low_groups(piece) * 4 : 0);
+        wlows = take(half && !forward ? (size_t)most_low_groups(piece) * 4 : 0);      // (the last piece may be shorter)
         least = take(half && !forward ? 8 : 0);
         pair = SM_NOTHING;
         top = label_out = dz = dz_dx = dxs = strips = partial = total = 0;

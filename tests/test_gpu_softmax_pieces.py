@@ -1,0 +1,26 @@
+"""Softmax cross-entropy whose classes are taken in pieces."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+pytest.importorskip("torch")
+from softmax_util import Reference, assert_within, grads, inputs  # noqa: E402
+from test_gpu_softmax import run_bwd  # noqa: E402
+
+
+@pytest.mark.parametrize("N,I,O", [(100, 6400, 8000), (512, 4096, 8000)])
+def test_a_short_last_piece_behind_a_long_one(N, I, O):
+    """fp32 weights of 4096 classes are laid out four rows a work-group, the 3904 of the last piece one by one: as many words of scratch for their exponents."""
+    x, w, b, labels, weight = inputs(N, I, O, 50, "f32")
+    ref = Reference(x, w, b, labels)
+    lse = ref.lse.astype(np.float32)
+    first = None
+    for _ in range(3):
+        got = run_bwd(N, I, O, "f32", x, w, b, labels, lse, weight, 1.0 / N, 0.0, None, None)
+        if first is None:
+            for k, (want, off) in grads(ref, lse, weight, "f32", 1.0 / N, 0.0, None, None).items():
+                assert_within(got[k], want, off, k)
+        else:
+            assert all(np.array_equal(first[k], got[k]) for k in got)
+        first = got
