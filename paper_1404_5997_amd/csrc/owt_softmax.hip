@@ -275,8 +275,8 @@ template <bool SCALED> __global__ void __launch_bounds__(256) sm_join_kernel(con
 __global__ void __launch_bounds__(256) softmax_join_kernel(int workers, int N, int classes, const float *lses, const float *targets, const int *labels,
                                                            float *lse, float *target, float *loss)
 {
-    const int n = blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
+    const unsigned n = blockIdx.x * 256 + threadIdx.x;      // (2^31 threads at most)
+    if (n >= (unsigned)N) return;
     if (!has_class(labels[n], classes)) {
         lse[n] = 0.f;
         if (target) target[n] = 0.f;
@@ -572,7 +572,7 @@ static void lay_tiles(SmParams &p, const SmPlan &pl)
     p.splits = pl.splits;
     p.steps_per_split = up(p.steps / p.products, pl.splits) * p.products;
 }
-static unsigned groups_of(size_t n, size_t most = 1u << 22)
+static unsigned groups_of(size_t n, size_t most)
 {
     const size_t g = (n + 255) / 256;
     return (unsigned)(g < most ? g : most);
@@ -947,7 +947,7 @@ owt_status owt_softmax_join(int workers, int N, int classes, const float *lses, 
     if (N == 0) return OWT_OK;
     OWT_TRY(need_ptr(lses, "lses")); OWT_TRY(need_ptr(targets, "targets")); OWT_TRY(need_ptr(labels, "labels")); OWT_TRY(need_ptr(lse, "lse"));
     OWT_TRY(may_ptr(target_or_null, "target")); OWT_TRY(may_ptr(loss_or_null, "loss"));
-    hipLaunchKernelGGL(softmax_join_kernel, dim3(groups_of(N)), dim3(256), 0, (hipStream_t)hip_stream, workers, N, classes, lses, targets, labels, lse,
+    hipLaunchKernelGGL(softmax_join_kernel, dim3(((unsigned)N + 255) / 256), dim3(256), 0, (hipStream_t)hip_stream, workers, N, classes, lses, targets, labels, lse,
                        target_or_null, loss_or_null);
     return launched();
 }
