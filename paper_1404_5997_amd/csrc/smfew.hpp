@@ -268,10 +268,14 @@ __global__ void __launch_bounds__(1024) sm_few_join_kernel(const SmFewParams f)
     if (wave || at >= n) return;
 #pragma unroll
     for (int k = 1; k < 16; k++) { sum.x += part[k][lane].x; sum.y += part[k][lane].y; sum.z += part[k][lane].z; sum.w += part[k][lane].w; }
+    // (a row without a class is zeros whatever w holds: its zeros of dz times an infinity are not)
+    float u[4];
+#pragma unroll
+    for (int t = 0; t < 4; t++) u[t] = at + t < n && has_class(f.p.labels[(unsigned)(at + t) / (unsigned)f.I], f.p.classes) ? sm_at(sum, t) : 0.f;
     float *to = (float *)f.p.out + at;
-    if (at + 4 <= n) *(float4 *)to = sum;
+    if (at + 4 <= n) *(float4 *)to = make_float4(u[0], u[1], u[2], u[3]);
     else
-        for (int t = 0; t < (int)(n - at); t++) to[t] = sm_at(sum, t);
+        for (int t = 0; t < (int)(n - at); t++) to[t] = sm_at(make_float4(u[0], u[1], u[2], u[3]), t);
 }
 
 }  // namespace owt
