@@ -336,7 +336,8 @@ size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass);     /* (
  * values (16 bits) or of two f16 ones, whatever dx is stored in; for dw it is the sum of three bf16 values (24 bits) where N I O_local <= 2^28 and
  * I O_local <= 2^24, or N <= 64.  f16 values of dz are under
  * one power of two for all rows: of exp(z - lse) and of 1 they hold 22 bits down to 2^-18, and 2^-40 below that (where rows of x, with their weights, or
- * of w differ in size, times the ratio of the largest row's largest magnitude to that of the row that is met, and up to four). */
+ * of w differ in size, times the ratio of the largest row's largest magnitude to that of the row that is met, and up to four).  exp(z - lse), which is 1 at
+ * most but for rounding errors of z, counts as 1.999 at most there. */
 
 /* Forward pass:  lse[n] = log sum_o exp z[n][o] (-infinity where every output is);  target[n] = z[n][label] if the label is one of this worker's
  * columns, else -infinity;  loss[n] = lse[n] - target[n] (+infinity for a class that is taken out).  All [N] fp32.  labels may be NULL (then target and

@@ -123,7 +123,9 @@ struct SmParams {
     float *partial;         // [splits][M][N] (splits > 1)
 };
 constexpr int kSmTop = 14;          // a row's largest magnitude is scaled to [2^14, 2^15)
-constexpr int kSmDzTop = 15;        // and dz to 2^15 for what is 1 with its factors (f16 values end at 2^16: exponentials may be up to 1.99)
+constexpr int kSmDzTop = 15;        // and dz to 2^15 for what is 1 with its factors
+// f16 values end at 65504: an exponential counts as this at most.  It is 1 at most but for the outputs' errors, which are that large for outputs from some 2^22 on.
+constexpr float kSmDzMost = 65504.f / 32768.f;
 constexpr int kSmNone = 1 << 20;    // the exponent of a row of zeros
 
 // What a row of dx is multiplied by: 0 without a class; with f16 values dz came without its weight
@@ -262,6 +264,7 @@ __device__ __forceinline__ void sm_dz(const SmParams &p, int2 least, int m, int 
     for (int t = 0; t < 4; t++) {
         const float from_lse = STARTED ? u[t] - 0.5f * w.lse : (SCALED ? ldexpf(u[t], -(w.exp + k.exp[t])) : u[t]) + k.bias[t] - w.lse;
         e[t] = w.weight == 0.f ? 0.f : exp_of(from_lse);        // (a row without a class may hold anything, and bf16 outputs are of x as it lies)
+        if (SCALED) e[t] = e[t] > kSmDzMost ? kSmDzMost : e[t];  // (NaN stays)
     }
     if (__any((unsigned)(w.label - c) < 4u))        // (of many classes hardly ever)
 #pragma unroll
