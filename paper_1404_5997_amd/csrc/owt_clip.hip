@@ -148,6 +148,15 @@ __global__ void __launch_bounds__(1024) grad_norm_join_kernel(const double *part
     if (threadIdx.x == 0) *norm = (float)sqrt(v);
 }
 
+// g times a factor is ((g * first) * second) * last.  A factor below 2^-100 (a bound of 0.001 on a norm of 1e30 is 2^-110) loses bits where fp32 has no normal number for it, though
+// what comes of a large g has all of its own: it goes in three parts then, of which only the last product may leave fp32's normal numbers.
+struct Factor { float first, second, last; };
+__device__ __forceinline__ Factor factor_of(double f)
+{
+    if (fabs(f) >= 0x1p-100) return {1.f, 1.f, (float)f};
+    return {0x1p-75f, (float)(f * 0x1p150), 0x1p-75f};
+}
+
 // out = g * min(1, max / norm); zeros where the norm is not finite.  Gradients that stay as they are and where they are are not touched.
 template <class T, bool PAST>
 __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, const float *norm, float max_norm)
@@ -155,18 +164,20 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, co
     constexpr int V = kPer<T>, CH = kChunkBytes / sizeof(T), U = CH / (V * 256);
     const float all = *norm;
     const bool fine = __builtin_isfinite(all);
-    const float factor = fine ? fminf(1.f, max_norm / all) : 0.f;
+    const double bounded = (double)max_norm / (double)all;
+    const bool whole = !(bounded < 1.);                     // (0 / 0 is no bound, either)
+    const Factor factor = factor_of(whole ? 1. : bounded);
     auto scaled = [&](const uint4 &v) __attribute__((always_inline)) {
         float f[V];
         widen<T>(v, f);
 #pragma unroll
-        for (int k = 0; k < V; k++) f[k] = fine ? f[k] * factor : 0.f;
+        for (int k = 0; k < V; k++) f[k] = fine ? f[k] * factor.first * factor.second * factor.last : 0.f;
         return narrow<T>(f);
     };
     walk_chunks<true>(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
         const T *g = (const T *)s.at[0][t] + from;
         T *out = (T *)s.at[1][t] + from;
-        if (factor == 1.f && g == out) return;
+        if (fine && whole && g == out) return;
         if (n == CH) {
             uint4 v[U];
 #pragma unroll
@@ -176,7 +187,7 @@ __global__ void __launch_bounds__(256) grad_clip_kernel(const TensorSet<2> s, co
         } else {
             for (unsigned i = threadIdx.x; i < n / V; i += 256) ((uint4 *)out)[i] = scaled(((const uint4 *)g)[i]);
             const unsigned i = n / V * V + threadIdx.x;
-            if (i < n) store1(out, i, fine ? load1(g, (int)i) * factor : 0.f);
+            if (i < n) store1(out, i, fine ? load1(g, (int)i) * factor.first * factor.second * factor.last : 0.f);
         }
     });
 }
@@ -190,9 +201,9 @@ __global__ void __launch_bounds__(256) sgd_clipped_kernel(const TensorSet<3 + CO
     const float all = *norm;
     if (!__builtin_isfinite(all)) return;
     const double bounded = (double)max_norm / ((double)fabsf(gscale) * (double)all);        // (0 / 0 is no bound, either)
-    const float scale = bounded < 1. ? (float)(gscale * bounded) : gscale;
+    const Factor scale = bounded < 1. ? factor_of(gscale * bounded) : Factor{1.f, 1.f, gscale};
     auto upd = [&](float &wv, float &vv, float gv) __attribute__((always_inline)) {
-        vv = fmaf(mu, vv, eps * fmaf(scale, gv, -omega * wv));
+        vv = fmaf(mu, vv, eps * fmaf(scale.last, gv * scale.first * scale.second, -omega * wv));
         wv += vv;
     };
     walk_chunks<true>(s, CH, [&](int t, size_t from, unsigned n) __attribute__((always_inline)) {
