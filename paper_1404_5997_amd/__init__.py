@@ -359,6 +359,15 @@ def owt_fc_softmax_bwd(desc, x, w, bias, labels, lse, weight_or_null, alpha, bet
                                    _ptr(dx_partial_or_null), _ptr(dw), _ptr(dbias_or_null), p, n, _stream(stream)))
 
 
+def _kind(t):
+    """A tensor's type by name; of what has none, the type that the library would take its values for."""
+    kind = getattr(t, "dtype", None)
+    return str(kind) if kind is not None else _KINDS.get({2: OWT_BF16, 4: OWT_F32}.get(t.element_size()))
+
+
+_KINDS = {OWT_F32: "torch.float32", OWT_BF16: "torch.bfloat16"}
+
+
 class tensor_list:
     """Tensors for the calls that take many: their pointers and sizes in the arrays that those calls read.  Made once, it keeps the tensors."""
 
@@ -366,8 +375,8 @@ class tensor_list:
         self.tensors = tuple(tensors)
         self.count = len(self.tensors)
         self.sizes = tuple(t.numel() for t in self.tensors)
-        self.width = self.tensors[0].element_size() if self.count else 0
-        if any(t.element_size() != self.width for t in self.tensors):
+        self.kind = _kind(self.tensors[0]) if self.count else None
+        if any(_kind(t) != self.kind for t in self.tensors):
             raise ValueError("the tensors of a list are of one type")
         self.at = (ctypes.c_void_p * max(1, self.count))(*[_ptr(t) for t in self.tensors])
         self.n = (ctypes.c_size_t * max(1, self.count))(*self.sizes)
@@ -375,13 +384,12 @@ class tensor_list:
 
 def _lists(dtype, first, others=(), copies=None):
     """Lists of one size and type (copies in bf16): what a call reads or writes of one has to exist in all."""
-    width = 2 if dtype == OWT_BF16 else 4
-    if first.count and first.width != width:
+    if first.count and dtype in _KINDS and first.kind != _KINDS[dtype]:
         raise ValueError("lists of other values than the call's")
     for l in others:
-        if l.sizes != first.sizes or l.width != first.width:
+        if l.sizes != first.sizes or l.kind != first.kind:
             raise ValueError("lists of different sizes or types")
-    if copies is not None and (copies.sizes != first.sizes or (copies.count and copies.width != 2)):
+    if copies is not None and (copies.sizes != first.sizes or (copies.count and copies.kind != _KINDS[OWT_BF16])):
         raise ValueError("copies of other sizes, or not in bf16")
 
 
