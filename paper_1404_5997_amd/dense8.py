@@ -4,7 +4,8 @@ A block is   h <- h + x;   u = relu(W1 norm(h) + b1);   x <- W2 u + b2   (x: wha
 output layer.  Weights live as fp32 masters and as 8-bit rows, which the products read and every update writes anew.
 
 The output layer's units are logistic, or a softmax over the classes.  A softmax is trained without its outputs: the loss and its gradients come from the
-normed rows and the layer's weights, both in storage type, so that no buffer has rows of `classes` values however many there are.  A bound on the
+normed rows and the layer's weights, both in storage type, so that no buffer has rows of `classes` values however many there are.  (The logits that
+`forward` gives come from the weights' 8-bit rows: a served probability differs from the trained one by what 8 bits leave out.)  A bound on the
 gradients' norm, where one is given, holds every step back to it.
 
 What a block keeps for its backward pass is h in storage type and, a byte a value, the 8-bit rows that its two products read: they are
@@ -50,9 +51,10 @@ class Dense8Stack:
             self.normed, self.lse = self._new((N, width)), self._new((N,), torch.float32)
         self._carve_parameters()
         self.grad_norm = self._new((1,), torch.float32)
-        self._lists = tuple(tensor_list([a]) for a in (self.params, self.vel, self.grads))
-        self._copies = tensor_list([self.copies]) if self.copies is not None else None
-        scratch = max(scratch, owt_grad_norm_workspace_bytes(self._lists[2]))
+        self._all_grads = tensor_list([self.grads])
+        self._lists = [tuple(tensor_list([a[lo:hi]]) for a in (self.params, self.vel, self.grads)) + (None if copy is None else tensor_list([copy]),)
+                       for lo, hi, copy in self._ranges]
+        scratch = max(scratch, owt_grad_norm_workspace_bytes(self._all_grads))
         self.ws = self._new((max(16, scratch),), torch.uint8)
         self.x = self._new((N, width))          # input, and what a block adds to h
         self.u, self.du = self._new((N, hidden)), self._new((N, hidden))        # one of each for all blocks
@@ -74,7 +76,7 @@ class Dense8Stack:
         return self._new((self.N, owt_q8_pitch(cols)), torch.int8)
 
     def _carve_parameters(self):
-        """Weights, biases and gains of the stack in one fp32 array, gradients and momentum in two more: the update is one launch."""
+        """Weights, biases and gains of the stack in one fp32 array, gradients and momentum in two more: the update is one launch, or two where a part has copies."""
         at, slots = 0, []
         for owner, name, shape in [(e, n, s) for e in self.layers for n, s in (("w", (e["O"], e["I"])), ("b", (e["O"],)))] + \
                                   [(b, "gain", (self.width,)) for b in self.blocks]:
@@ -82,12 +84,18 @@ class Dense8Stack:
             slots.append((owner, name, shape, at, n))
             at += (n + 7) // 8 * 8              # every view 16-byte aligned
         self.params, self.grads, self.vel = (torch.zeros((at,), device="cuda", dtype=torch.float32) for _ in range(3))
-        # a softmax reads its layer's weights in storage type: in bf16 every update writes a copy
-        self.copies = torch.zeros((at,), device="cuda", dtype=torch.bfloat16) if self.softmax and self.tdt == torch.bfloat16 else None
         for owner, name, shape, o, n in slots:
-            if name == "w" and owner is self.layers[-1]:
-                owner["stored"] = (self.params if self.copies is None else self.copies)[o:o + n].view(shape)
             owner[name], owner["d" + name] = self.params[o:o + n].view(shape), self.grads[o:o + n].view(shape)
+        # A softmax reads its layer's weights in storage type: in bf16 every update writes a copy, from those weights on to the array's end (biases and gains).
+        head = self.layers[-1]
+        self.copies, self._ranges = None, [(0, at, None)]
+        if self.softmax and self.tdt == torch.bfloat16:
+            o, n = next((o, n) for owner, name, _, o, n in slots if owner is head and name == "w")
+            self.copies = torch.zeros((at - o,), device="cuda", dtype=torch.bfloat16)
+            self._ranges = [(0, o, None)] * (o > 0) + [(o, at, self.copies)]
+            head["stored"] = self.copies[:n].view(head["w"].shape)
+        else:
+            head["stored"] = head["w"]
 
     def init(self, seed):
         g = torch.Generator(device="cuda").manual_seed(seed)
@@ -100,8 +108,9 @@ class Dense8Stack:
 
     def pack_weights(self):
         """8-bit rows, and copies in storage type, of the masters as they are."""
-        if self.copies is not None:
-            self.copies.copy_(self.params)
+        for lo, hi, copy in self._ranges:
+            if copy is not None:
+                copy.copy_(self.params[lo:hi])
         self._pack_rows()
 
     def _pack_rows(self):
@@ -172,11 +181,12 @@ class Dense8Stack:
 
     def update(self, mu, eps, omega):
         if self.max_norm is None:
-            owt_sgd_momentum_update(self.params.numel(), self.params, self.vel, self.grads, mu, eps, omega, -1.0, self.copies)
+            for lo, hi, copy in self._ranges:
+                owt_sgd_momentum_update(hi - lo, self.params[lo:hi], self.vel[lo:hi], self.grads[lo:hi], mu, eps, omega, -1.0, copy)
         else:
-            w, vel, g = self._lists
-            owt_grad_norm(g, OWT_F32, self.grad_norm, self.ws)
-            owt_sgd_momentum_clipped(w, vel, g, mu, eps, omega, -1.0, self.grad_norm, self.max_norm, self._copies)
+            owt_grad_norm(self._all_grads, OWT_F32, self.grad_norm, self.ws)
+            for w, vel, g, copy in self._lists:
+                owt_sgd_momentum_clipped(w, vel, g, mu, eps, omega, -1.0, self.grad_norm, self.max_norm, copy)
         self._pack_rows()
 
     def step(self, x, labels, mu=0.9, eps=0.01, omega=0.0005):
