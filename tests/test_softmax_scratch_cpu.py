@@ -54,3 +54,7 @@ def test_a_short_last_piece_behind_a_long_one(layouts):
     for c, w in zip(cases, layouts(cases)):
         assert w.startswith("ok"), (c, w)
         assert int(w.split()[2]) >= 4096 > int(w.split()[3]), (c, w)
+
+
+def test_sizes_that_the_forward_pass_takes_in_pieces(layouts):
+    assert layouts([(1, 1, 65, 8192, 9000), (0, 1, 65, 8193, 17000)]) == ["ok 2 4608 4392", "ok 2 8704 8296"]
