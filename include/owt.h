@@ -328,7 +328,8 @@ size_t owt_fc_shard_q8_workspace_bytes(const owt_fc_desc *d, int pass);     /* (
  * are never stored whole: the columns are taken in pieces.  x [N][I] and w [O_local][I] in the descriptor's dtype, bias fp32, read only with
  * OWT_BIAS (the only flag).  labels [N]: class index in the whole layer.  A row whose label is outside [0, O_total) has no class: it is padding,
  * whatever its x holds (infinities and NaN, too) has no influence on any other row, its lse, target, loss and dx are 0.
- * A bias of -infinity takes a class out: it adds nothing to lse and gets no gradient.  N == 0 is an empty batch.
+ * A bias of -infinity takes a class out: it adds nothing to lse and gets no gradient but from rows that have it as their label (dz is -weight there, as
+ * exp(z - lse) is 0).  N == 0 is an empty batch.
  * N, I, O_local <= 2^22, x and w of at most 2^31-1 values, no more tiles of outputs than a launch counts (OWT_EUNSUPPORTED).
  *
  * bf16 operands are multiplied as they are.  fp32 ones may be multiplied as sums of two f16 values under a power of two for each row of x and of w,
