@@ -409,7 +409,7 @@ static bool sm_few(bool half, bool forward, int N, int I, int ol)
 
 // dx takes dz in two bf16 values, 16 bits of it, in every bf16 layer.  A row's dz add up to zero, so that what all classes' weights have in common cancels in dx, and what one value
 // loses, 2^-9 of each term, does not: where the weights differ by a 32nd of their size one value left dx off by 40 to 70 times what its sums and its own rounding explain.
-// us with two (one): 16 x 2048 -> 65536 284 (247), 777 x 1537 -> 20011 363 (321), 4096 x 4096 -> 65536 8450 (7090).
+// us with two (one): 16 x 2048 -> 65536 268 (247), 777 x 1537 -> 20011 363 (321), 4096 x 4096 -> 65536 8450 (7090).
 // dw takes it in three, all its 24 bits, in bf16 layers of up to so many products, and a sixteenth as many weights, where launches are most of what it costs: dw of 15 x 192
 // -> 512 is off by 5.4e-7 of its size then (2.2e-6 with two).  Rows of one step, up to 64, take three, too, as their sums are too short to lose as much themselves.  A quarter of the
 // time of larger layers would be for what their outputs' own sums lose.
@@ -472,6 +472,10 @@ struct SmLayout {
             z = sm_plan(N, cols, isteps * products, products, forward ? SM_TOP : SM_DZ);
             if (forward) return;
             dx = sm_plan(N, I, up(cols, 64) * products_x, products_x, SM_OUT);
+            // 64 x 64 results of two products read w for each: a second work-group on the CU hides what the first waits for (us with one and two: 16 x 2048 -> 65536 84 and 71,
+            // 1 x 2048 -> 65536 83 and 55, 64 x 4096 -> 32768 88 and 86, 40 x 1024 -> 10000 10.7 and 10.3)
+            const long groups = dx.tile == SM_SMALL && !half && forced_split() <= 0 ? (long)up(N, 64) * up(I, 64) * dx.splits : 0;
+            if (groups > 128 && groups <= 256 && dx.splits * 4 <= up(cols, 64)) dx.splits *= 2;
             // (few rows of many weights: the third product is behind the results' writing, 16 x 2048 -> 65536 148 us, 161 where the tile is chosen for it)
             const int shown = planes == 3 && (double)I * ol > kSmLittle / 16 ? SM_PAIR : products_w;
             dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * shown, shown, SM_OUT);
