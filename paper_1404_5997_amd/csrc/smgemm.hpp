@@ -21,8 +21,8 @@
 //
 // fp32 values are two f16 ones, of the value times 2^e, e of its row: the row's largest magnitude then lies in [2^14, 2^15).  A result's sums are of values
 // times 2^(e of its row + e of its column).
-// What bounds it: power on large products, 1.31 PFLOP/s with the forward pass's end (8192 rows 4096 -> 32768 in 1680 us, the library's product alone runs at
-// 1.31), 1.39 for dw's pairs, 1.15 where outputs leave as dz (a tenth of a tile's time is its end: 16 K exponentials a wavefront, two bf16 values each).  Few
+// What bounds it: power on large products, 1.22 to 1.31 PFLOP/s with the forward pass's end (8192 rows 4096 -> 32768 in 1680 to 1800 us, the library's product alone
+// runs at 1.31), 1.39 for dw's pairs, 1.30 for dx's, 1.15 where outputs leave as dz (a tenth of a tile's time is its end: 16 K exponentials a wavefront, two bf16 values each).  Few
 // rows: memory (one row 4096 -> 65536 104 us, 5.4 TB/s of weights).  256 x 256 results a work-group of four wavefronts read 64 bytes a clock from LDS for 512 clocks of
 // the matrix unit a slice, half of what LDS gives; smaller tiles read more and serve sizes with few tiles.
 #pragma once
