@@ -473,9 +473,11 @@ struct SmLayout {
             if (forward) return;
             dx = sm_plan(N, I, up(cols, 64) * products_x, products_x, SM_OUT);
             // 64 x 64 results of two products read w for each: a second work-group on the CU hides what the first waits for (us with one and two: 16 x 2048 -> 65536 84 and 71,
-            // 1 x 2048 -> 65536 83 and 55, 64 x 4096 -> 32768 88 and 86, 40 x 1024 -> 10000 10.7 and 10.3)
+            // 1 x 2048 -> 65536 83 and 55, 64 x 4096 -> 32768 88 and 86, 40 x 1024 -> 10000 10.7 and 10.3).  Not where its sums get shorter than eight steps of memory, the first
+            // join is for less than 32, or more than 32 parts are joined (us of the whole pass with one and two: 3 x 784 -> 8393 41.4 and 42.0, 200 x 4096 -> 1024 42.4 and 45.0,
+            // 28 x 347 -> 32768 69.9 and 73.7; 96 x 2048 -> 4345 51.1 and 48.7, 250 x 4000 -> 2048 70.5 and 68.6, 1316 x 192 -> 12742 100.8 and 92.4)
             const long groups = dx.tile == SM_SMALL && !half && forced_split() <= 0 ? (long)up(N, 64) * up(I, 64) * dx.splits : 0;
-            if (groups > 128 && groups <= 256 && dx.splits * 4 <= up(cols, 64)) dx.splits *= 2;
+            if (groups > 128 && groups <= 256 && dx.splits <= 16 && up(cols, 64) / dx.splits >= (dx.splits > 1 ? 16 : 32)) dx.splits *= 2;
             // (few rows of many weights: the third product is behind the results' writing, 16 x 2048 -> 65536 148 us, 161 where the tile is chosen for it)
             const int shown = planes == 3 && (double)I * ol > kSmLittle / 16 ? SM_PAIR : products_w;
             dw = sm_plan(cols, I, up(N > 0 ? N : 1, 64) * shown, shown, SM_OUT);
