@@ -409,7 +409,7 @@ static bool sm_few(bool half, bool forward, int N, int I, int ol)
 
 // dx takes dz in two bf16 values, 16 bits of it, in every bf16 layer.  A row's dz add up to zero, so that what all classes' weights have in common cancels in dx, and what one value
 // loses, 2^-9 of each term, does not: where the weights differ by a 32nd of their size one value left dx off by 40 to 70 times what its sums and its own rounding explain.
-// us with two (one): 16 x 2048 -> 65536 268 (247), 777 x 1537 -> 20011 363 (321), 4096 x 4096 -> 65536 8450 (7090).
+// us with two (one): 16 x 2048 -> 65536 262 (247), 777 x 1537 -> 20011 363 (321), 4096 x 4096 -> 65536 8450 (7090).
 // dw takes it in three, all its 24 bits, in bf16 layers of up to so many products, and a sixteenth as many weights, where launches are most of what it costs: dw of 15 x 192
 // -> 512 is off by 5.4e-7 of its size then (2.2e-6 with two).  Rows of one step, up to 64, take three, too, as their sums are too short to lose as much themselves.  A quarter of the
 // time of larger layers would be for what their outputs' own sums lose.
